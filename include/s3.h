@@ -42,13 +42,17 @@ enum {
     S3_ERR_STATE = -7         /* call not allowed in the object's current state                    */
 };
 
-typedef enum { S3_BF16 = 0, S3_F32 = 1 } s3_dtype;
+typedef enum { S3_BF16 = 0, S3_F32 = 1, S3_F16 = 2 /* key / value caches only */ } s3_dtype;
 
 #define S3_MAX_K 128           /* largest Top-k per token                                           */
 #define S3_MAX_POSTINGS_ITEMS 32
 #define S3_MAX_ENCODE_ITEMS 8    /* encoder calls one grouped launch can serve                        */
 #define S3_MAX_SCORE_LAYERS 16
 #define S3_WS_HEADER_BYTES 64
+#define S3_MAX_HEAD_GROUP 128    /* query heads per key head                                          */
+#define S3_MAX_BLOCK_LIST 512    /* blocks in one list of s3_block_attention                          */
+#define S3_MAX_SELECT 64         /* blocks s3_block_select may choose per token and key head          */
+#define S3_MAX_SELECT_BLOCKS 16384 /* blocks of one sequence it can choose from                       */
 
 const char* s3_last_error(void);
 int s3_version(void);
@@ -535,6 +539,118 @@ s3_status s3_fuse_index_sets(const int32_t* d_centers, int Q, int n_centers, int
                              const int32_t* d_lexical /*nullable*/, int n_lex, int lead, int tail, int64_t L,
                              int32_t* d_out_idx /*[Q,cap]*/, int cap, int32_t* d_out_count /*[Q]*/,
                              void* d_ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * Paged key / value cache: append, block selection, attention
+ *            (the paper's model side: Alg. 1 Phase 1 runs the LLM over one chunk at a time, Phase 3 answers from the
+ *             retained evidence. These calls give a program that attention: over a chunk while it is scanned, over a cache
+ *             token by token, and over the evidence blocks only, whether a cheap score picks them per token or the span
+ *             retrieval returns them per query. Span width 64 = a page of 64 positions.)
+ *
+ * Cache: two arrays of n_pages pages, a page [n_kv_heads, page_size, head_dim] contiguous, pages *_page_stride elements
+ * apart (so keys and values may interleave page by page in one pool). S3_BF16 or S3_F16; head_dim 64 or 128; page_size
+ * 16, 32, 64 or 128; n_kv_heads <= 65535; page strides multiples of 8. d_code / d_scale (both or neither) hold per page and
+ * head the summary of the block's keys: int8 [n_pages, n_kv_heads, head_dim] and fp32 [n_pages, n_kv_heads],
+ *   S[d]  = sum over the block's positions of rint(4096 * clamp(k[d], -2047, 2047))      (int32, NaN counts as 0)
+ *   code  = rint(127 * S[d] / max_d |S[d]|),  scale = max_d |S[d]| / number of positions
+ * (code * scale / (127 * 4096) is the mean key). Integer sums: a summary does not depend on the order of the additions.
+ * The handle is host memory only (the arrays stay the caller's).
+ *
+ * Batch: n_seqs sequences whose new tokens are packed in T rows. Sequence i has rows [d_cu_q[i], d_cu_q[i+1]) (cu_q[0] = 0,
+ * cu_q[n_seqs] = T, zero rows allowed), d_kv_len[i] cached positions, its new tokens included and last: its row r
+ * has position kv_len - n + r. Block j of the sequence (positions [j, j+1) * page_size) lies in page
+ * d_pages[i * ld_pages + j]. max_q / max_kv are host-known upper bounds of new rows / cached positions per sequence;
+ * max_kv <= ld_pages * page_size. Lengths outside the bounds are cut to them, and a page outside [0, n_pages) is neither
+ * read nor written (it reads as zeros); both are reported through the workspace status as S3_ERR_INVALID_ARG.
+ *
+ * What a call never uses, whatever it holds (NaN too): positions >= kv_len, pages and blocks that are not listed, table
+ * entries past the length. Keys that a row may not see do not enter its result; VALUES at positions < kv_len of a block that
+ * the call reads must be finite (a zero weight times an infinity is a NaN).
+ *
+ * All row pitches are in elements, multiples of 8, heads contiguous within a row (a slice of a fused projection will do);
+ * pointers 16-byte aligned. One workspace of s3_kv_workspace_bytes() serves every call below.
+ * ---------------------------------------------------------------------------------------------- */
+typedef struct s3_kv_cache s3_kv_cache;
+typedef struct {
+    void* d_k;
+    void* d_v;
+    int64_t k_page_stride, v_page_stride;
+    int8_t* d_code;      /* nullable */
+    float* d_scale;      /* nullable */
+    int32_t n_pages, n_kv_heads, page_size, head_dim;
+    s3_dtype dtype;
+    int32_t reserved;
+} s3_kv_cache_desc;
+
+typedef struct {
+    const int32_t* d_cu_q;
+    const int32_t* d_kv_len;
+    const int32_t* d_pages;
+    int64_t ld_pages;
+    int32_t n_seqs, T, max_q, max_kv;
+} s3_kv_batch;
+
+s3_status s3_kv_cache_create(s3_kv_cache** out, const s3_kv_cache_desc* desc);
+s3_status s3_kv_cache_destroy(s3_kv_cache* cache);
+/* Scratch that suffices for every call over this batch (or one with smaller bounds) with n_heads query heads. */
+size_t s3_kv_workspace_bytes(const s3_kv_cache* cache, const s3_kv_batch* batch, int n_heads);
+
+/* Append: the keys d_k [T, n_kv_heads, head_dim] of the new tokens are rotated and written, the values d_v copied, to their
+ * positions' slots (a row whose position is negative is not stored); the queries d_q [T, n_heads, head_dim] (nullable) are
+ * rotated into d_q_out (which may be d_q); when the cache has summaries, those of every block that holds a new token
+ * are computed afresh from the block's positions < kv_len as the cache then holds them.
+ * Rotation (rope nullable = none) by the angle table's row p, p = d_positions[t] (nullable: the cached position): pairs
+ * (x[i], x[i + rot_dim/2]), or (x[2i], x[2i+1]) when interleaved, i < rot_dim/2, become
+ * (x0 cos[p,i] - x1 sin[p,i], x1 cos[p,i] + x0 sin[p,i]), each product and sum rounded in fp32, the result once to the
+ * cache's type; dimensions past rot_dim are copied. cos / sin fp32 [n_pos, rot_dim/2]; rot_dim a multiple of 16. A p outside
+ * [0, n_pos) uses the nearest row and is reported through the workspace status. */
+typedef struct {
+    const float* d_cos;
+    const float* d_sin;
+    int32_t n_pos, rot_dim, interleaved, reserved;
+} s3_rope;
+
+s3_status s3_kv_append(const s3_kv_cache* cache, const s3_kv_batch* batch, const s3_rope* rope /*nullable*/,
+                       const int32_t* d_positions /*[T] nullable*/, const void* d_q /*nullable*/, int64_t ldq, int n_heads,
+                       void* d_q_out, int64_t ld_qo, const void* d_k, int64_t ldk, const void* d_v, int64_t ldv,
+                       void* d_ws, size_t ws_bytes, void* stream);
+
+/* Block selection: for every new token at position p and key head, the s blocks among 0 .. p/page_size that are the first
+ * n_first, the last n_last, or else have the highest scores (ties: the lower block), ascending, padded with -1:
+ *   Q[d] = sum over the key head's query heads of rint(4096 * clamp(q[d], -2047, 2047)),  c = rint(127 * Q / max|Q|)
+ *   score(j) = fl32( sum_d c[d] code_j[d] ) * scale_j                    (one rounding of an exact integer sum)
+ * which ranks blocks by the group's summed query times the block's mean key, both in 8 bits: the result is a function of the
+ * inputs alone, not of the order of the additions. A token at a negative position gets no blocks. Needs the summaries.
+ * Limits: 1 <= s <= S3_MAX_SELECT, n_first + n_last <= s, max_kv <= S3_MAX_SELECT_BLOCKS * page_size. */
+s3_status s3_block_select(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* d_q, int64_t ldq, int n_heads, int s,
+                          int n_first, int n_last, int32_t* d_blocks /*[T, n_kv_heads, s]*/, void* d_ws, size_t ws_bytes,
+                          void* stream);
+
+/* Attention of the new tokens over the cache (their own keys appended before): for row t at position p and query head h, over
+ * the visible positions j (j <= p if causal, else all; j > p - window if window > 0),
+ *   out[t,h] = sum_j exp(scale q.k_j - m) v_j / sum_j exp(scale q.k_j - m),   lse[t,h] = ln sum_j exp(scale q.k_j)
+ * Query head h reads key head h / (n_heads / n_kv_heads). A row that sees nothing gives 0 and lse -inf. Products of the
+ * cache's type accumulated in fp32, softmax statistics in fp32, the weights rounded to the cache's type for the second
+ * product, the result rounded once. Without causal, p counts as kv_len - 1 for every row.
+ * Limits: n_heads a multiple of n_kv_heads, at most S3_MAX_HEAD_GROUP times it. */
+typedef struct {
+    float scale;
+    int32_t causal, window;    /* window 0 = unlimited */
+    int32_t reserved;
+} s3_attn_params;
+
+s3_status s3_paged_attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* d_q, int64_t ldq, int n_heads,
+                             const s3_attn_params* params, void* d_out /*[T, n_heads, head_dim]*/, int64_t ld_out,
+                             float* d_lse /*[T, n_heads] nullable*/, void* d_ws, size_t ws_bytes, void* stream);
+
+/* The same over listed blocks only: d_blocks holds one list of s block numbers per token ([T, list_heads, s], per_token = 1) or
+ * per sequence ([n_seqs, list_heads, s], shared by the sequence's new tokens: the layout of the spans that
+ * s3_coactivation_score_topspans returns at width = stride = page_size), list_heads being n_kv_heads or 1 (shared by the
+ * heads). Any order; entries < 0 or past the sequence's blocks are skipped; a block must not be listed twice.
+ * s <= S3_MAX_BLOCK_LIST. */
+s3_status s3_block_attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* d_q, int64_t ldq, int n_heads,
+                             const int32_t* d_blocks, int s, int list_heads, int per_token, const s3_attn_params* params,
+                             void* d_out, int64_t ld_out, float* d_lse /*nullable*/, void* d_ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

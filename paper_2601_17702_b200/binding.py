@@ -14,7 +14,7 @@ LIB_PATH = os.path.join(_HERE, "libs3scan.so")
 S3_OK = 0
 S3_ERR_INVALID_ARG, S3_ERR_UNSUPPORTED, S3_ERR_CUDA, S3_ERR_NOMEM = -1, -2, -3, -4
 S3_ERR_CAPACITY, S3_ERR_TIMEOUT, S3_ERR_STATE = -5, -6, -7
-S3_BF16, S3_F32 = 0, 1
+S3_BF16, S3_F32, S3_F16 = 0, 1, 2
 S3_SCORE_MINCOUNT, S3_SCORE_WEIGHTED = 0, 1
 S3_WS_HEADER_BYTES = 64
 S3_MAX_ENCODE_ITEMS = 8
@@ -37,6 +37,8 @@ EXPORTS = [
     "s3_compact_save", "s3_compact_file_info", "s3_compact_load",
     "s3_sae_decode", "s3_head_aggregate_topk", "s3_compact_expand",
     "s3_sae_backward_workspace_bytes", "s3_sae_backward", "s3_adam_update", "s3_cast_f32_to_bf16", "s3_sae_preact",
+    "s3_kv_cache_create", "s3_kv_cache_destroy", "s3_kv_workspace_bytes", "s3_kv_append", "s3_block_select", "s3_paged_attention",
+    "s3_block_attention",
 ]
 
 
@@ -76,6 +78,26 @@ class AdamParams(C.Structure):
                 ("reserved", C.c_int32)]
 
 
+class KvCacheDesc(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("k_page_stride", C.c_int64), ("v_page_stride", C.c_int64),
+                ("d_code", C.c_void_p), ("d_scale", C.c_void_p), ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("page_size", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class KvBatchDesc(C.Structure):
+    _fields_ = [("d_cu_q", C.c_void_p), ("d_kv_len", C.c_void_p), ("d_pages", C.c_void_p), ("ld_pages", C.c_int64),
+                ("n_seqs", C.c_int32), ("T", C.c_int32), ("max_q", C.c_int32), ("max_kv", C.c_int32)]
+
+
+class RopeDesc(C.Structure):
+    _fields_ = [("d_cos", C.c_void_p), ("d_sin", C.c_void_p), ("n_pos", C.c_int32), ("rot_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("reserved", C.c_int32)]
+
+
+class AttnParams(C.Structure):
+    _fields_ = [("scale", C.c_float), ("causal", C.c_int32), ("window", C.c_int32), ("reserved", C.c_int32)]
+
+
 class ScoreParams(C.Structure):
     _fields_ = [("width", C.c_int32), ("stride", C.c_int32), ("mode", C.c_int32), ("s", C.c_int32),
                 ("alpha", C.c_float), ("beta", C.c_float), ("stop_freq", C.c_int64)]
@@ -106,7 +128,7 @@ def lib():
         for name in ("s3_sae_prepared_bytes", "s3_sae_encode_workspace_bytes", "s3_postings_workspace_bytes",
                      "s3_score_workspace_bytes", "s3_density_workspace_bytes", "s3_fuse_workspace_bytes",
                      "s3_compact_workspace_bytes", "s3_sae_backward_workspace_bytes", "s3_sae_encode_grouped_workspace_bytes",
-                     "s3_sae_project_encode_workspace_bytes"):
+                     "s3_sae_project_encode_workspace_bytes", "s3_kv_workspace_bytes"):
             getattr(L, name).restype = C.c_size_t
         L.s3_sae_prepared_bytes.argtypes = [C.c_int, C.c_int, C.c_int]
         L.s3_sae_create.argtypes = [C.POINTER(C.c_void_p), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int,
@@ -176,6 +198,14 @@ def lib():
         L.s3_adam_update.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.POINTER(AdamParams), C.c_void_p]
         L.s3_sae_preact.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_size_t,
                                     C.c_void_p]
+        P, I, N = C.c_void_p, C.c_int, C.c_int64
+        L.s3_kv_cache_create.argtypes = [C.POINTER(C.c_void_p), C.POINTER(KvCacheDesc)]
+        L.s3_kv_cache_destroy.argtypes = [P]
+        L.s3_kv_workspace_bytes.argtypes = [P, C.POINTER(KvBatchDesc), I]
+        L.s3_kv_append.argtypes = [P, C.POINTER(KvBatchDesc), C.POINTER(RopeDesc), P, P, N, I, P, N, P, N, P, N, P, C.c_size_t, P]
+        L.s3_block_select.argtypes = [P, C.POINTER(KvBatchDesc), P, N, I, I, I, I, P, P, C.c_size_t, P]
+        L.s3_paged_attention.argtypes = [P, C.POINTER(KvBatchDesc), P, N, I, C.POINTER(AttnParams), P, N, P, P, C.c_size_t, P]
+        L.s3_block_attention.argtypes = [P, C.POINTER(KvBatchDesc), P, N, I, P, I, I, I, C.POINTER(AttnParams), P, N, P, P, C.c_size_t, P]
         _lib = L
     return _lib
 
@@ -715,3 +745,169 @@ def s3_sae_preact(sae: "Sae", x: torch.Tensor, out_dtype: torch.dtype = torch.fl
     _check(lib().s3_sae_preact(sae.handle, _ptr(x), x.stride(0) if T > 1 else max(x.stride(0), sae.d_in), T, _ptr(out), out.stride(0),
                                code, _ptr(ws), ws.numel(), _stream(stream)))
     return out
+
+
+# ------------------------------------------------------------------------------------------------ paged key / value cache
+_KV_DTYPES = {torch.bfloat16: S3_BF16, torch.float16: S3_F16}
+
+
+class KvCache:
+    """Handle of a paged key / value cache (s3_kv_cache_create / s3_kv_cache_destroy) over the caller's tensors, which it keeps
+    alive: k, v [n_pages, n_kv_heads, page_size, head_dim] bf16 or f16, contiguous within a page (so two views of one pool
+    will do), code int8 [n_pages, n_kv_heads, head_dim] and scale fp32 [n_pages, n_kv_heads] for the block summaries, or
+    neither."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, code: torch.Tensor | None = None, scale: torch.Tensor | None = None):
+        assert k.is_cuda and v.is_cuda and k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype
+        n_pages, H, P, D = k.shape
+        for t in (k, v):
+            assert t[0].is_contiguous()
+        assert (code is None) == (scale is None)
+        if code is not None:
+            assert code.dtype == torch.int8 and code.is_contiguous() and tuple(code.shape) == (n_pages, H, D)
+            assert scale.dtype == torch.float32 and scale.is_contiguous() and tuple(scale.shape) == (n_pages, H)
+        self.k, self.v, self.code, self.scale = k, v, code, scale
+        self.n_pages, self.n_kv_heads, self.page_size, self.head_dim, self.dtype = n_pages, H, P, D, k.dtype
+        p = lambda t: None if t is None else t.data_ptr()
+        stride = lambda t: t.stride(0) if n_pages > 1 else H * P * D
+        desc = KvCacheDesc(p(k), p(v), stride(k), stride(v), p(code), p(scale), n_pages, H, P, D, _KV_DTYPES.get(k.dtype, -1), 0)
+        h = C.c_void_p()
+        _check(lib().s3_kv_cache_create(C.byref(h), C.byref(desc)))
+        self.handle = h
+
+    @classmethod
+    def zeros(cls, n_pages: int, n_kv_heads: int, page_size: int, head_dim: int, dtype=torch.bfloat16, summaries: bool = True,
+              device="cuda"):
+        k = torch.zeros((n_pages, n_kv_heads, page_size, head_dim), dtype=dtype, device=device)
+        code = torch.zeros((n_pages, n_kv_heads, head_dim), dtype=torch.int8, device=device) if summaries else None
+        scale = torch.zeros((n_pages, n_kv_heads), dtype=torch.float32, device=device) if summaries else None
+        return cls(k, torch.zeros_like(k), code, scale)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().s3_kv_cache_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class KvBatch:
+    """The sequences of one step: cu_q int32 [n+1], kv_len int32 [n], pages int32 [n, blocks] on the device, T = cu_q[n] packed
+    rows, max_q / max_kv host-known bounds of the rows and cached positions of a sequence. One object serves every layer of
+    the step."""
+
+    def __init__(self, cu_q: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor, T: int, max_q: int, max_kv: int):
+        n = kv_len.numel()
+        assert cu_q.dtype == kv_len.dtype == pages.dtype == torch.int32
+        assert cu_q.is_cuda and kv_len.is_cuda and pages.is_cuda
+        assert cu_q.is_contiguous() and kv_len.is_contiguous() and cu_q.numel() == n + 1
+        assert pages.dim() == 2 and pages.shape[0] == n and (pages.shape[1] <= 1 or pages.stride(1) == 1)
+        assert n <= 1 or pages.stride(0) >= pages.shape[1]
+        self.cu_q, self.kv_len, self.pages, self.T, self.max_q, self.max_kv = cu_q, kv_len, pages, T, max_q, max_kv
+        self.n_seqs, self.blocks = n, pages.shape[1]
+        # a single row may have any pitch: what counts is how many entries it has
+        self.desc = KvBatchDesc(cu_q.data_ptr(), kv_len.data_ptr(), pages.data_ptr(), pages.stride(0) if n > 1 else pages.shape[1], n, T,
+                                max_q, max_kv)
+        self.ref = C.byref(self.desc)
+
+
+class Rope:
+    """Rotation tables cos / sin fp32 [n_pos, rot_dim / 2], row = position; interleaved pairs (2i, 2i+1) or halves (i, i + rot_dim/2)."""
+
+    def __init__(self, cos: torch.Tensor, sin: torch.Tensor, interleaved: bool = False):
+        assert cos.is_cuda and sin.is_cuda and cos.dtype == sin.dtype == torch.float32 and cos.shape == sin.shape and cos.dim() == 2
+        assert cos.is_contiguous() and sin.is_contiguous()
+        self.cos, self.sin = cos, sin
+        self.desc = RopeDesc(cos.data_ptr(), sin.data_ptr(), cos.shape[0], 2 * cos.shape[1], int(interleaved), 0)
+        self.ref = C.byref(self.desc)
+
+
+def _rows(t: torch.Tensor, cache: KvCache, T: int, heads: int | None = None) -> int:
+    """Row pitch of a [T, heads, head_dim] tensor whose heads are contiguous."""
+    D = cache.head_dim
+    assert t.is_cuda and t.dtype == cache.dtype and t.dim() == 3 and t.shape[0] == T and t.shape[2] == D
+    assert heads is None or t.shape[1] == heads
+    s = t.stride()
+    assert s[2] == 1 and (s[1] == D or t.shape[1] == 1)
+    return s[0] if T > 1 else max(s[0], t.shape[1] * D + 7 & ~7)
+
+
+def s3_kv_workspace_bytes(cache: KvCache, batch: KvBatch, n_heads: int) -> int:
+    return int(lib().s3_kv_workspace_bytes(cache.handle, batch.ref, n_heads))
+
+
+def s3_kv_append(cache: KvCache, batch: KvBatch, k: torch.Tensor, v: torch.Tensor, ws: torch.Tensor, q: torch.Tensor | None = None,
+                 rope: Rope | None = None, positions: torch.Tensor | None = None, q_out: torch.Tensor | None = None, stream=None):
+    """Rotates and writes the new tokens' keys k [T, n_kv_heads, head_dim], copies their values v, brings the summaries of the
+    touched blocks up to date, and returns the rotated queries (None without q; q_out may be q). positions int32 [T]: rows of
+    the rotation tables, where they are not the cached positions."""
+    T = batch.T
+    assert batch.max_kv <= batch.blocks * cache.page_size
+    ldk, ldv = _rows(k, cache, T, cache.n_kv_heads), _rows(v, cache, T, cache.n_kv_heads)
+    assert positions is None or (positions.is_cuda and positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == T)
+    ldq = ld_qo = n_heads = 0
+    if q is not None:
+        n_heads, ldq = q.shape[1], _rows(q, cache, T)
+        if q_out is None:
+            q_out = torch.empty((T, n_heads, cache.head_dim), dtype=q.dtype, device=q.device)
+        ld_qo = _rows(q_out, cache, T, n_heads)
+    _check(lib().s3_kv_append(cache.handle, batch.ref, None if rope is None else rope.ref, None if positions is None else positions.data_ptr(),
+                              None if q is None else q.data_ptr(), ldq, n_heads, None if q is None else q_out.data_ptr(), ld_qo,
+                              k.data_ptr(), ldk, v.data_ptr(), ldv, ws.data_ptr(), ws.numel(), _stream(stream)))
+    return q_out if q is not None else None
+
+
+def s3_block_select(cache: KvCache, batch: KvBatch, q: torch.Tensor, s: int, ws: torch.Tensor, n_first: int = 1, n_last: int = 2,
+                    blocks: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """blocks int32 [T, n_kv_heads, s]: per token (rotated query q [T, n_heads, head_dim]) and key head the blocks to attend to."""
+    assert batch.max_kv <= batch.blocks * cache.page_size
+    ldq = _rows(q, cache, batch.T)
+    if blocks is None:
+        blocks = torch.empty((batch.T, cache.n_kv_heads, s), dtype=torch.int32, device=q.device)
+    assert blocks.dtype == torch.int32 and blocks.is_contiguous() and tuple(blocks.shape) == (batch.T, cache.n_kv_heads, s)
+    _check(lib().s3_block_select(cache.handle, batch.ref, q.data_ptr(), ldq, q.shape[1], s, n_first, n_last, blocks.data_ptr(),
+                                 ws.data_ptr(), ws.numel(), _stream(stream)))
+    return blocks
+
+
+def _attention_rows(cache, batch, q, out, lse, want_lse):
+    assert batch.max_kv <= batch.blocks * cache.page_size
+    ldq = _rows(q, cache, batch.T)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    ld_out = _rows(out, cache, batch.T, q.shape[1])
+    if lse is None and want_lse:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+    assert lse is None or (lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2])
+    return ldq, out, ld_out, lse
+
+
+def s3_paged_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, ws: torch.Tensor, scale: float | None = None, causal: bool = True,
+                       window: int = 0, out: torch.Tensor | None = None, lse: torch.Tensor | None = None, want_lse: bool = False,
+                       stream=None):
+    """Attention of the new tokens' rotated queries q [T, n_heads, head_dim] over the cache (their keys appended before). Returns
+    (out like q, lse fp32 [T, n_heads] or None). scale defaults to head_dim ** -0.5."""
+    ldq, out, ld_out, lse = _attention_rows(cache, batch, q, out, lse, want_lse)
+    params = AttnParams(cache.head_dim ** -0.5 if scale is None else scale, int(causal), window, 0)
+    _check(lib().s3_paged_attention(cache.handle, batch.ref, q.data_ptr(), ldq, q.shape[1], C.byref(params), out.data_ptr(), ld_out,
+                                    None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)))
+    return out, lse
+
+
+def s3_block_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, blocks: torch.Tensor, ws: torch.Tensor, scale: float | None = None,
+                       causal: bool = True, window: int = 0, per_token: bool = True, out: torch.Tensor | None = None,
+                       lse: torch.Tensor | None = None, want_lse: bool = False, stream=None):
+    """The same over listed blocks: blocks int32 [T, n_kv_heads or 1, s] (per_token; e.g. s3_block_select) or
+    [n_seqs, n_kv_heads or 1, s] (one list per sequence; e.g. the top spans of s3_coactivation_score_topspans, unsqueezed)."""
+    ldq, out, ld_out, lse = _attention_rows(cache, batch, q, out, lse, want_lse)
+    assert blocks.is_cuda and blocks.dtype == torch.int32 and blocks.is_contiguous() and blocks.dim() == 3
+    assert blocks.shape[0] == (batch.T if per_token else batch.n_seqs)
+    params = AttnParams(cache.head_dim ** -0.5 if scale is None else scale, int(causal), window, 0)
+    _check(lib().s3_block_attention(cache.handle, batch.ref, q.data_ptr(), ldq, q.shape[1], blocks.data_ptr(), blocks.shape[2],
+                                    blocks.shape[1], int(per_token), C.byref(params), out.data_ptr(), ld_out,
+                                    None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel(), _stream(stream)))
+    return out, lse

@@ -106,6 +106,9 @@ s3_status s3_workspace_status(const void* d_ws, void* stream, uint32_t* code_out
     if (code == DEV_BAD_FEATURE_ID) return fail(S3_ERR_INVALID_ARG, "a feature id >= d_sae was met on the device (code %u)", code);
     if (code == DEV_DUPLICATE_ID) return fail(S3_ERR_INVALID_ARG, "a token carried the same feature id twice (code %u)", code);
     if (code == DEV_COMPACT_CAPACITY) return fail(S3_ERR_CAPACITY, "compact index: block or payload buffer too small (code %u)", code);
+    if (code == DEV_BAD_BATCH) return fail(S3_ERR_INVALID_ARG, "a sequence exceeds the batch's max_q, max_kv or T (code %u)", code);
+    if (code == DEV_BAD_PAGE) return fail(S3_ERR_INVALID_ARG, "a block table names a page outside the cache (code %u)", code);
+    if (code == DEV_BAD_POSITION) return fail(S3_ERR_INVALID_ARG, "a position lies outside the rotation table (code %u)", code);
     return fail(S3_ERR_TIMEOUT, "a bounded device-side wait ran out (code %u)", code);
 }
 

@@ -43,6 +43,9 @@ enum : uint32_t {
     DEV_BAD_FEATURE_ID = 16,     // postings: id >= d_sae met in the input
     DEV_COMPACT_CAPACITY = 17,   // compact index: block or payload buffer too small (sizes[] has the need)
     DEV_DUPLICATE_ID = 18,       // postings: one token carries the same feature id twice
+    DEV_BAD_BATCH = 32,          // key / value cache: a sequence's lengths exceed the batch's bounds
+    DEV_BAD_PAGE = 33,           // key / value cache: a page number outside the cache
+    DEV_BAD_POSITION = 34,       // key / value cache: a position outside the rotation table
 };
 
 __device__ __forceinline__ void dev_set_error(uint32_t* status, uint32_t code) { atomicCAS(status, 0u, code); }

@@ -103,4 +103,18 @@ s3_status launch_density(const s3_csr_view* h_layers, int n_layers, int d_sae, i
                          int64_t stop_freq, int32_t* d_centers, float* d_center_density, float* d_s_out, float* d_d_out,
                          void* d_scratch, cudaStream_t stream);
 
+// Paged key / value cache (see s3_kv.cuh for the structs).
+struct KvCacheState;
+struct KvBatchDev;
+struct AttnArgs;
+s3_status make_kv_query_map(unsigned char (&map)[128], const KvCacheState& c, const void* d_q, int64_t ldq, int T, int group, int box_tokens);
+s3_status launch_kv_append(const KvCacheState& c, const KvBatchDev& b, const s3_rope* rope, const int32_t* d_positions,
+                           const void* d_q, int64_t ldq, int n_heads, void* d_q_out, int64_t ld_qo, const void* d_k, int64_t ldk,
+                           const void* d_v, int64_t ldv, uint32_t* d_status, cudaStream_t stream);
+s3_status launch_block_select(const KvCacheState& c, const KvBatchDev& b, const void* d_q, int64_t ldq, int n_heads, int s,
+                              int n_first, int n_last, int32_t* d_blocks, uint32_t* d_status, cudaStream_t stream);
+s3_status launch_attn_split(const KvCacheState& c, const AttnArgs& a, cudaStream_t stream);   // at most 16 query rows per item
+s3_status launch_attn_tile(const KvCacheState& c, const AttnArgs& a, cudaStream_t stream);    // tiles of 128 query rows
+s3_status launch_attn_join(const KvCacheState& c, const AttnArgs& a, cudaStream_t stream);    // joins the splits of either
+
 }  // namespace s3

@@ -1,0 +1,360 @@
+// C ABI of the paged key / value cache: argument checks, the cache handle with its copy descriptors, and the choice of kernel
+// and splits for attention.
+#include <math.h>
+#include <string.h>
+
+#include <new>
+
+#include "s3_kernels.cuh"
+#include "s3_kv.cuh"
+
+namespace s3 {
+namespace {
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+s3_status encode_fn(EncodeTiledFn* out)
+{
+    static EncodeTiledFn fn = nullptr;
+    if (!fn) {
+        void* sym = nullptr;
+        cudaDriverEntryPointQueryResult qres;
+        S3_CUDA_TRY(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &sym, cudaEnableDefault, &qres));
+        S3_REQUIRE(sym != nullptr && qres == cudaDriverEntryPointSuccess, S3_ERR_CUDA, "the driver does not provide cuTensorMapEncodeTiled");
+        fn = reinterpret_cast<EncodeTiledFn>(sym);
+    }
+    *out = fn;
+    return S3_OK;
+}
+
+// 4-D map (column, row, head, page or token) of 16-bit values; strides in elements; box 64 columns wide, 128-byte swizzle.
+s3_status make_map(unsigned char (&map)[128], s3_dtype dtype, const void* base, const uint64_t (&dims)[4], const uint64_t (&strides)[3],
+                   uint32_t box_rows, uint32_t box_last)
+{
+    static_assert(sizeof(CUtensorMap) == 128, "a copy descriptor has 128 bytes");
+    EncodeTiledFn fn;
+    const s3_status st = encode_fn(&fn);
+    if (st != S3_OK) return st;
+    const cuuint64_t d[4] = {dims[0], dims[1], dims[2], dims[3]};
+    const cuuint64_t s[3] = {strides[0] * 2, strides[1] * 2, strides[2] * 2};
+    const cuuint32_t box[4] = {64, box_rows, 1, box_last}, unit[4] = {1, 1, 1, 1};
+    const CUresult r = fn(reinterpret_cast<CUtensorMap*>(map), dtype == S3_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                          4, const_cast<void*>(base), d, s, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    S3_REQUIRE(r == CUDA_SUCCESS, S3_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", static_cast<int>(r));
+    return S3_OK;
+}
+
+constexpr int kSplitRows = 16;             // rows per item up to which the split kernel serves
+constexpr int kTileRows = 128;
+constexpr int kMaxSplits = 256;
+
+// How an attention call is cut: which kernel, tokens per item, items, and the most splits it may use. None of it depends on the
+// device-side lengths, so the same numbers size the workspace.
+struct AttnPlan {
+    bool tile;
+    int tok_per_item, n_items, one_item_per_seq, max_splits;
+};
+
+AttnPlan plan_attention(const s3_kv_batch& b, int group, int n_kv_heads, bool list_per_token)
+{
+    AttnPlan p;
+    const int n_sm = device_sm_count();
+    if (list_per_token) {
+        p.tile = group > kSplitRows;
+        p.tok_per_item = 1;
+        p.n_items = b.T;
+        p.one_item_per_seq = 0;
+    } else {
+        p.tile = static_cast<int64_t>(b.max_q) * group > kSplitRows;
+        const int one = (p.tile ? kTileRows : kSplitRows) / group;
+        p.tok_per_item = p.tile && b.max_q > one ? 2 * one : one;
+        p.one_item_per_seq = b.max_q <= p.tok_per_item;
+        p.n_items = p.one_item_per_seq ? b.n_seqs : b.T / p.tok_per_item + b.n_seqs;
+    }
+    // Splits fill the SMs when there are few items: up to eight thread blocks per SM in the split kernel (two run at a time; the
+    // rest evens out sequences of unequal length), two in the tile kernel (one runs at a time).
+    const int64_t blocks = static_cast<int64_t>(p.n_items) * n_kv_heads;
+    const int64_t want = (static_cast<int64_t>(p.tile ? 2 : 8) * n_sm + blocks - 1) / (blocks > 0 ? blocks : 1);
+    p.max_splits = static_cast<int>(want < 1 ? 1 : want > kMaxSplits ? kMaxSplits : want);
+    return p;
+}
+
+size_t partial_bytes(const s3_kv_batch& b, int n_heads, int head_dim, int n_splits)
+{
+    if (n_splits <= 1) return 0;
+    const size_t rows = static_cast<size_t>(b.T) * n_heads * n_splits;
+    return round_up(rows * head_dim * 4, 256) + round_up(rows * 4, 256);
+}
+
+}  // namespace
+
+s3_status make_kv_query_map(unsigned char (&map)[128], const KvCacheState& c, const void* d_q, int64_t ldq, int T, int group, int box_tokens)
+{
+    const uint64_t D = c.d.head_dim;
+    const uint64_t dims[4] = {D, static_cast<uint64_t>(group), static_cast<uint64_t>(c.d.n_kv_heads), static_cast<uint64_t>(T)};
+    const uint64_t strides[3] = {D, D * group, static_cast<uint64_t>(ldq)};
+    return make_map(map, c.d.dtype, d_q, dims, strides, static_cast<uint32_t>(group), static_cast<uint32_t>(box_tokens));
+}
+
+}  // namespace s3
+
+using namespace s3;
+
+struct s3_kv_cache {
+    KvCacheState st;
+};
+
+namespace {
+
+s3_status check_batch(const s3_kv_cache* cache, const s3_kv_batch* b)
+{
+    S3_REQUIRE(cache != nullptr && b != nullptr, S3_ERR_INVALID_ARG, "cache or batch is null");
+    S3_REQUIRE(b->n_seqs >= 0 && b->T >= 0 && b->max_q >= 0 && b->max_kv >= 0 && b->ld_pages >= 0, S3_ERR_INVALID_ARG,
+               "n_seqs = %d, T = %d, max_q = %d, max_kv = %d, ld_pages = %lld out of range", b->n_seqs, b->T, b->max_q, b->max_kv,
+               (long long)b->ld_pages);
+    if (b->T == 0 || b->n_seqs == 0) return S3_OK;
+    S3_REQUIRE(b->d_cu_q && b->d_kv_len && b->d_pages, S3_ERR_INVALID_ARG, "null pointer in the batch");
+    S3_REQUIRE(static_cast<int64_t>(b->max_kv) <= b->ld_pages * cache->st.d.page_size, S3_ERR_INVALID_ARG,
+               "max_kv = %d does not fit %lld table entries of %d positions", b->max_kv, (long long)b->ld_pages, cache->st.d.page_size);
+    S3_REQUIRE(b->max_q >= 1 && b->max_q <= b->T, S3_ERR_INVALID_ARG, "max_q = %d out of [1, T = %d]", b->max_q, b->T);
+    S3_REQUIRE(b->max_kv <= (1 << 30) && b->T <= (1 << 30), S3_ERR_UNSUPPORTED, "more than 2^30 positions or rows");
+    return S3_OK;
+}
+
+s3_status check_heads(const s3_kv_cache* cache, int n_heads)
+{
+    const int k = cache->st.d.n_kv_heads;
+    S3_REQUIRE(n_heads >= 1 && n_heads % k == 0, S3_ERR_INVALID_ARG, "n_heads = %d is not a multiple of %d key heads", n_heads, k);
+    S3_REQUIRE(n_heads / k <= S3_MAX_HEAD_GROUP, S3_ERR_UNSUPPORTED, "%d query heads per key head exceed %d", n_heads / k, S3_MAX_HEAD_GROUP);
+    return S3_OK;
+}
+
+s3_status check_rows(const char* what, const void* p, int64_t ld, int heads, int dim)
+{
+    S3_REQUIRE(p != nullptr && aligned16(p), S3_ERR_INVALID_ARG, "%s is null or misaligned", what);
+    S3_REQUIRE(ld % 8 == 0 && ld >= static_cast<int64_t>(heads) * dim, S3_ERR_INVALID_ARG,
+               "%s: row pitch %lld must be a multiple of 8 and at least %d", what, (long long)ld, heads * dim);
+    S3_REQUIRE(ld < (int64_t(1) << 38), S3_ERR_UNSUPPORTED, "%s: row pitch %lld is too large", what, (long long)ld);
+    return S3_OK;
+}
+
+#define S3_TRY(expr)                      \
+    do {                                  \
+        const s3_status st__ = (expr);    \
+        if (st__ != S3_OK) return st__;   \
+    } while (0)
+
+KvBatchDev device_batch(const s3_kv_batch& b)
+{
+    return KvBatchDev{b.d_cu_q, b.d_kv_len, b.d_pages, b.ld_pages, b.n_seqs, b.T, b.max_q, b.max_kv};
+}
+
+s3_status attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* d_q, int64_t ldq, int n_heads,
+                    const int32_t* d_blocks, int s, int list_heads, int list_mode, const s3_attn_params* params, void* d_out,
+                    int64_t ld_out, float* d_lse, void* d_ws, size_t ws_bytes, void* stream)
+{
+    S3_TRY(check_batch(cache, batch));
+    S3_TRY(check_heads(cache, n_heads));
+    S3_REQUIRE(params != nullptr, S3_ERR_INVALID_ARG, "params is null");
+    S3_REQUIRE(isfinite(params->scale) && params->scale > 0.0f, S3_ERR_INVALID_ARG, "scale must be positive and finite");
+    S3_REQUIRE(params->window >= 0, S3_ERR_INVALID_ARG, "window = %d is negative", params->window);
+    const KvCacheState& c = cache->st;
+    const s3_kv_batch& b = *batch;
+    if (b.T == 0 || b.n_seqs == 0) return S3_OK;
+    S3_TRY(check_rows("d_q", d_q, ldq, n_heads, c.d.head_dim));
+    S3_TRY(check_rows("d_out", d_out, ld_out, n_heads, c.d.head_dim));
+    S3_REQUIRE(d_ws != nullptr && ws_bytes >= S3_WS_HEADER_BYTES, S3_ERR_CAPACITY, "workspace missing or smaller than %d bytes", S3_WS_HEADER_BYTES);
+    const int group = n_heads / c.d.n_kv_heads;
+    const AttnPlan p = plan_attention(b, group, c.d.n_kv_heads, list_mode == LIST_PER_TOKEN);
+
+    AttnArgs a;
+    memset(&a, 0, sizeof(a));
+    a.b = device_batch(b);
+    a.n_heads = n_heads;
+    a.n_kv_heads = c.d.n_kv_heads;
+    a.group = group;
+    a.page_size = c.d.page_size;
+    a.page_shift = c.page_shift;
+    a.box_rows = c.box_rows;
+    a.n_pages = c.d.n_pages;
+    a.head_dim = c.d.head_dim;
+    a.scale = params->scale;
+    a.scale_log2 = params->scale * kLog2e;
+    a.causal = params->causal != 0;
+    a.window = params->window;
+    a.lists = d_blocks;
+    a.s = s;
+    a.list_heads = list_heads;
+    a.list_mode = list_mode;
+    a.q = d_q;
+    a.ldq = ldq;
+    a.out = d_out;
+    a.ld_out = ld_out;
+    a.lse = d_lse;
+    a.tok_per_item = p.tok_per_item;
+    a.n_items = p.n_items;
+    a.one_item_per_seq = p.one_item_per_seq;
+    a.status = static_cast<uint32_t*>(d_ws);
+
+    // Virtual keys of the longest item, cut into splits of whole tiles that are not worth cutting further.
+    const int tile = p.tile ? 128 : 64, least = p.tile ? 512 : 256;
+    int64_t keys = list_mode == LIST_NONE ? b.max_kv : static_cast<int64_t>(s) << c.page_shift;
+    if (list_mode == LIST_NONE && params->window > 0) {
+        const int64_t seen = static_cast<int64_t>(params->window) + p.tok_per_item + tile;
+        if (seen < keys) keys = seen;
+    }
+    int64_t len = (keys + p.max_splits - 1) / p.max_splits;
+    if (len < least) len = least;
+    len = (len + tile - 1) / tile * tile;
+    a.split_len = static_cast<int32_t>(len);
+    a.n_splits = static_cast<int32_t>((keys + len - 1) / len);
+    if (a.n_splits < 1) a.n_splits = 1;
+    const size_t need = 256 + partial_bytes(b, n_heads, c.d.head_dim, a.n_splits);
+    S3_REQUIRE(a.n_splits == 1 || ws_bytes >= need, S3_ERR_CAPACITY, "workspace holds %zu bytes, %zu needed", ws_bytes, need);
+    if (a.n_splits > 1) {
+        const size_t rows = static_cast<size_t>(b.T) * n_heads * a.n_splits;
+        a.part_o = reinterpret_cast<float*>(static_cast<unsigned char*>(d_ws) + 256);
+        a.part_lse = reinterpret_cast<float*>(static_cast<unsigned char*>(d_ws) + 256 + round_up(rows * c.d.head_dim * 4, 256));
+    }
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    S3_TRY(p.tile ? launch_attn_tile(c, a, st) : launch_attn_split(c, a, st));
+    return a.n_splits > 1 ? launch_attn_join(c, a, st) : S3_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+s3_status s3_kv_cache_create(s3_kv_cache** out, const s3_kv_cache_desc* desc)
+{
+    S3_REQUIRE(out != nullptr, S3_ERR_INVALID_ARG, "out is null");
+    *out = nullptr;
+    S3_REQUIRE(desc != nullptr, S3_ERR_INVALID_ARG, "desc is null");
+    const s3_kv_cache_desc& d = *desc;
+    S3_REQUIRE(d.d_k && d.d_v && aligned16(d.d_k) && aligned16(d.d_v), S3_ERR_INVALID_ARG, "key or value pages are null or misaligned");
+    S3_REQUIRE((d.d_code != nullptr) == (d.d_scale != nullptr), S3_ERR_INVALID_ARG, "summaries need codes and scales");
+    S3_REQUIRE(aligned16(d.d_code) && aligned16(d.d_scale), S3_ERR_INVALID_ARG, "summary arrays must be 16-byte aligned");
+    S3_REQUIRE(d.dtype == S3_BF16 || d.dtype == S3_F16, S3_ERR_UNSUPPORTED, "a cache holds bf16 or f16 (got dtype %d)", (int)d.dtype);
+    S3_REQUIRE(d.n_pages >= 1 && d.n_kv_heads >= 1 && d.n_kv_heads <= 65535, S3_ERR_INVALID_ARG, "n_pages = %d, n_kv_heads = %d out of range",
+               d.n_pages, d.n_kv_heads);
+    S3_REQUIRE(d.head_dim == 64 || d.head_dim == 128, S3_ERR_UNSUPPORTED, "head_dim = %d (64 or 128)", d.head_dim);
+    S3_REQUIRE(d.page_size == 16 || d.page_size == 32 || d.page_size == 64 || d.page_size == 128, S3_ERR_UNSUPPORTED,
+               "page_size = %d (16, 32, 64 or 128)", d.page_size);
+    const int64_t page = static_cast<int64_t>(d.n_kv_heads) * d.page_size * d.head_dim;
+    S3_REQUIRE(d.k_page_stride >= page && d.v_page_stride >= page && d.k_page_stride % 8 == 0 && d.v_page_stride % 8 == 0, S3_ERR_INVALID_ARG,
+               "page strides %lld, %lld must be multiples of 8 and at least %lld", (long long)d.k_page_stride, (long long)d.v_page_stride,
+               (long long)page);
+    S3_REQUIRE(d.k_page_stride < (int64_t(1) << 38) && d.v_page_stride < (int64_t(1) << 38), S3_ERR_UNSUPPORTED, "page stride too large");
+    int n_dev = 0;
+    S3_CUDA_TRY(cudaGetDeviceCount(&n_dev));
+    S3_REQUIRE(device_cc_major() == 10, S3_ERR_UNSUPPORTED, "this library runs on sm_100 devices only (found compute capability %d.x)",
+               device_cc_major());
+    s3_kv_cache* c = new (std::nothrow) s3_kv_cache;
+    S3_REQUIRE(c != nullptr, S3_ERR_NOMEM, "out of host memory");
+    c->st.d = d;
+    c->st.page_shift = d.page_size == 16 ? 4 : d.page_size == 32 ? 5 : d.page_size == 64 ? 6 : 7;
+    c->st.box_rows = d.page_size < 64 ? d.page_size : 64;
+    const uint64_t D = d.head_dim, P = d.page_size;
+    const uint64_t dims[4] = {D, P, static_cast<uint64_t>(d.n_kv_heads), static_cast<uint64_t>(d.n_pages)};
+    const uint64_t ks[3] = {D, D * P, static_cast<uint64_t>(d.k_page_stride)}, vs[3] = {D, D * P, static_cast<uint64_t>(d.v_page_stride)};
+    s3_status st = make_map(c->st.map_k, d.dtype, d.d_k, dims, ks, c->st.box_rows, 1);
+    if (st == S3_OK) st = make_map(c->st.map_v, d.dtype, d.d_v, dims, vs, c->st.box_rows, 1);
+    if (st != S3_OK) {
+        delete c;
+        return st;
+    }
+    *out = c;
+    return S3_OK;
+}
+
+s3_status s3_kv_cache_destroy(s3_kv_cache* cache)
+{
+    delete cache;
+    return S3_OK;
+}
+
+size_t s3_kv_workspace_bytes(const s3_kv_cache* cache, const s3_kv_batch* batch, int n_heads)
+{
+    if (check_batch(cache, batch) != S3_OK || check_heads(cache, n_heads) != S3_OK) return 0;
+    size_t most = 0;
+    if (batch->T > 0 && batch->n_seqs > 0)
+        for (int per_token = 0; per_token < 2; ++per_token) {
+            const AttnPlan p = plan_attention(*batch, n_heads / cache->st.d.n_kv_heads, cache->st.d.n_kv_heads, per_token != 0);
+            const size_t bytes = partial_bytes(*batch, n_heads, cache->st.d.head_dim, p.max_splits);
+            if (bytes > most) most = bytes;
+        }
+    return 256 + most;
+}
+
+s3_status s3_kv_append(const s3_kv_cache* cache, const s3_kv_batch* batch, const s3_rope* rope, const int32_t* d_positions,
+                       const void* d_q, int64_t ldq, int n_heads, void* d_q_out, int64_t ld_qo, const void* d_k, int64_t ldk,
+                       const void* d_v, int64_t ldv, void* d_ws, size_t ws_bytes, void* stream)
+{
+    S3_TRY(check_batch(cache, batch));
+    const KvCacheState& c = cache->st;
+    if (rope) {
+        S3_REQUIRE(rope->rot_dim >= 0 && rope->rot_dim <= c.d.head_dim, S3_ERR_INVALID_ARG, "rot_dim = %d out of [0, %d]", rope->rot_dim, c.d.head_dim);
+        S3_REQUIRE(rope->rot_dim % 16 == 0, S3_ERR_UNSUPPORTED, "rot_dim = %d must be a multiple of 16", rope->rot_dim);
+        if (rope->rot_dim > 0) {
+            S3_REQUIRE(rope->d_cos && rope->d_sin && aligned16(rope->d_cos) && aligned16(rope->d_sin), S3_ERR_INVALID_ARG,
+                       "rotation tables are null or misaligned");
+            S3_REQUIRE(rope->n_pos >= 1, S3_ERR_INVALID_ARG, "the rotation tables are empty");
+        }
+    }
+    if (d_q) S3_TRY(check_heads(cache, n_heads));
+    if (batch->T == 0 || batch->n_seqs == 0) return S3_OK;
+    if (d_q) {
+        S3_TRY(check_rows("d_q", d_q, ldq, n_heads, c.d.head_dim));
+        S3_TRY(check_rows("d_q_out", d_q_out, ld_qo, n_heads, c.d.head_dim));
+    }
+    S3_TRY(check_rows("d_k", d_k, ldk, c.d.n_kv_heads, c.d.head_dim));
+    S3_TRY(check_rows("d_v", d_v, ldv, c.d.n_kv_heads, c.d.head_dim));
+    S3_REQUIRE(d_ws != nullptr && ws_bytes >= S3_WS_HEADER_BYTES, S3_ERR_CAPACITY, "workspace missing or smaller than %d bytes", S3_WS_HEADER_BYTES);
+    return launch_kv_append(c, device_batch(*batch), rope, d_positions, d_q, ldq, n_heads, d_q_out, ld_qo, d_k, ldk, d_v, ldv,
+                            static_cast<uint32_t*>(d_ws), static_cast<cudaStream_t>(stream));
+}
+
+s3_status s3_block_select(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* d_q, int64_t ldq, int n_heads, int s,
+                          int n_first, int n_last, int32_t* d_blocks, void* d_ws, size_t ws_bytes, void* stream)
+{
+    S3_TRY(check_batch(cache, batch));
+    S3_TRY(check_heads(cache, n_heads));
+    const KvCacheState& c = cache->st;
+    S3_REQUIRE(c.d.d_code != nullptr, S3_ERR_STATE, "the cache was created without summaries");
+    S3_REQUIRE(s >= 1 && n_first >= 0 && n_last >= 0, S3_ERR_INVALID_ARG, "s = %d, n_first = %d, n_last = %d out of range", s, n_first, n_last);
+    S3_REQUIRE(s <= S3_MAX_SELECT, S3_ERR_UNSUPPORTED, "s = %d exceeds %d", s, S3_MAX_SELECT);
+    S3_REQUIRE(n_first <= s && n_last <= s && n_first + n_last <= s, S3_ERR_INVALID_ARG, "n_first + n_last exceeds s = %d", s);
+    S3_REQUIRE(batch->max_kv <= static_cast<int64_t>(S3_MAX_SELECT_BLOCKS) * c.d.page_size, S3_ERR_UNSUPPORTED, "max_kv = %d exceeds %d blocks",
+               batch->max_kv, S3_MAX_SELECT_BLOCKS);
+    if (batch->T == 0 || batch->n_seqs == 0) return S3_OK;
+    S3_TRY(check_rows("d_q", d_q, ldq, n_heads, c.d.head_dim));
+    S3_REQUIRE(d_blocks != nullptr, S3_ERR_INVALID_ARG, "d_blocks is null");
+    S3_REQUIRE(d_ws != nullptr && ws_bytes >= S3_WS_HEADER_BYTES, S3_ERR_CAPACITY, "workspace missing or smaller than %d bytes", S3_WS_HEADER_BYTES);
+    return launch_block_select(c, device_batch(*batch), d_q, ldq, n_heads, s, n_first, n_last, d_blocks, static_cast<uint32_t*>(d_ws),
+                               static_cast<cudaStream_t>(stream));
+}
+
+s3_status s3_paged_attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* d_q, int64_t ldq, int n_heads,
+                             const s3_attn_params* params, void* d_out, int64_t ld_out, float* d_lse, void* d_ws, size_t ws_bytes, void* stream)
+{
+    return attention(cache, batch, d_q, ldq, n_heads, nullptr, 0, 1, LIST_NONE, params, d_out, ld_out, d_lse, d_ws, ws_bytes, stream);
+}
+
+s3_status s3_block_attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* d_q, int64_t ldq, int n_heads,
+                             const int32_t* d_blocks, int s, int list_heads, int per_token, const s3_attn_params* params, void* d_out,
+                             int64_t ld_out, float* d_lse, void* d_ws, size_t ws_bytes, void* stream)
+{
+    S3_REQUIRE(cache != nullptr, S3_ERR_INVALID_ARG, "cache is null");
+    S3_REQUIRE(s >= 1, S3_ERR_INVALID_ARG, "s = %d out of range", s);
+    S3_REQUIRE(s <= S3_MAX_BLOCK_LIST, S3_ERR_UNSUPPORTED, "s = %d exceeds %d", s, S3_MAX_BLOCK_LIST);
+    S3_REQUIRE(list_heads == 1 || list_heads == cache->st.d.n_kv_heads, S3_ERR_INVALID_ARG, "list_heads = %d (1 or %d)", list_heads,
+               cache->st.d.n_kv_heads);
+    S3_REQUIRE(d_blocks != nullptr || (batch && (batch->T == 0 || batch->n_seqs == 0)), S3_ERR_INVALID_ARG, "d_blocks is null");
+    return attention(cache, batch, d_q, ldq, n_heads, d_blocks, s, list_heads, per_token ? LIST_PER_TOKEN : LIST_PER_SEQ, params, d_out, ld_out,
+                     d_lse, d_ws, ws_bytes, stream);
+}
+
+}  // extern "C"
