@@ -1,13 +1,19 @@
 // Attention of a few query rows (at most 16 per item and key head) over a paged cache: decoding steps and lists per token.
 //
-//   out = sum_j p_j v_j / sum_j p_j,  p_j = 2^(scale log2e q.k_j - m)      one pass, running maximum m and sum
+//   out = sum_j p_j v_j / sum_j p_j,  p_j = 2^(scale log2e q.k_j - m)      one pass, running reference m and sum
 //
-// Bound by reading keys and values once (HBM, or the L2 cache when neighbouring tokens list the same blocks). A thread block
-// takes one (item, key head, split of the keys). Warp 4 copies 64-key tiles of K and V with TMA, page by page, into a ring of
-// STAGES shared-memory slots; warps 0-3 take 16 keys of every tile each and keep their own m, sum and 16 x head_dim
-// accumulator in registers, so the warps meet only at the end. Both products run on mma.sync m16n8k16 with the rows padded
-// to 16: with this few rows per key the work is a copy, and the padding costs nothing that the memory would not.
-// The four partial results, and then the splits (second kernel), are joined by their maxima and sums.
+// Bound by reading keys and values once (HBM, or the L2 cache when tokens list the same blocks). Two persistent thread blocks
+// per SM walk the work (units of one item and one key head, or pieces of them). Warp 4 reads a unit's lengths, list and table entries, copies its
+// query rows and then its 64-key tiles of K and V (TMA, page by page) into a ring of shared-memory slots, and goes on to the next
+// unit while the others still compute: a unit's start (four dependent reads before the first key arrives, about 5 us with one
+// thread block per unit) and its end (joining the warps) hide behind the copies.
+// Warps 0-3 take 16 keys of every tile each and keep their own reference, sum and accumulator in registers, so the warps meet
+// only at the end of a unit. Both products are taken transposed, S^T = K Q^T and O^T = V^T P^T (mma.sync m16n8k16): the 16-wide
+// side of the instruction holds keys and dimensions, the 8-wide side the query rows, of which a group of 4 or 7 fills most.
+// P^T changes its fragment form in registers (movmatrix). The reference moves only when a score exceeds it by 2^8, which one
+// warp vote decides; weights then stay below 2^8, inside either type. With this few rows per key the work is a copy.
+#include <string.h>
+
 #include <type_traits>
 
 #include "s3_kernels.cuh"
@@ -19,18 +25,32 @@ namespace {
 using namespace kv;
 
 constexpr int TILE = 64;                  // keys per tile
-constexpr int STAGES = 3;
 constexpr int WARPS = 4;                  // compute warps
 constexpr int THREADS = 32 * (WARPS + 1);
+constexpr float RESCALE_AT = 8.0f;
 
 struct Maps {
     alignas(64) unsigned char k[128], v[128];
 };
 
-template <int D>
-__host__ __device__ constexpr int stage_bytes() { return 2 * TILE * D * 2; }
-template <int D>
-constexpr size_t smem_bytes() { return 1024 + static_cast<size_t>(STAGES) * stage_bytes<D>() + S3_MAX_BLOCK_LIST * 4; }
+// What the producer tells the compute warps about a unit.
+struct UnitInfo {
+    int rows, n_tiles, tok0, pos0, pos_last, kv, head, slot;       // rows 0: no more units
+};
+
+// NT: groups of 8 query rows. Two thread blocks per SM have 113 KB of shared memory each.
+template <int D, int NT>
+struct Layout {
+    static constexpr int STAGE = 2 * TILE * D * 2;
+    static constexpr int STAGES = (D == 128 ? 3 : 6) - (NT == 2 ? 1 : 0) * (D == 128 ? 1 : 2);
+    static constexpr int PITCH = D + 4;                              // floats; rows of two lanes of a quad fall 8 banks apart
+    static constexpr int Q_PITCH = D * 2 + 16;                       // bytes
+    static constexpr int SLOTS = STAGES * STAGE;                     // two accumulators on their way to another warp
+    static constexpr int SLOT = NT * 8 * PITCH * 4;
+    static constexpr int Q = SLOTS + 2 * SLOT;
+    static constexpr int TOTAL = Q + 2 * NT * 8 * Q_PITCH;
+    static_assert(TOTAL + 1024 + 1024 <= 114 * 1024, "two thread blocks per SM");
+};
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr)
 {
@@ -42,6 +62,12 @@ __device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr)
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
+__device__ __forceinline__ uint32_t transpose8(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
 template <class T>
 __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
@@ -52,340 +78,482 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-
-template <class T, int D>
-__global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant__ Maps maps, const AttnArgs a)
+// Untiled copy of bytes (a multiple of 16, both addresses on 16-byte boundaries) into this block's shared memory.
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar)
 {
-    extern __shared__ unsigned char smem_raw[];
-    unsigned char* ring = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    int* list = reinterpret_cast<int*>(ring + STAGES * stage_bytes<D>());
-    __shared__ uint64_t full_bar[STAGES], empty_bar[STAGES];
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)), "l"(src),
+                 "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+
+template <class T, int D, int NT>
+__global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant__ Maps maps, const __grid_constant__ AttnArgs a)
+{
+    using L = Layout<D, NT>;
+    constexpr int STAGES = L::STAGES;
+    extern __shared__ __align__(1024) unsigned char ring[];           // swizzled tiles start on 1024-byte boundaries
+    __shared__ uint64_t full_bar[STAGES], empty_bar[STAGES], unit_full[2], unit_empty[2];
+    __shared__ uint64_t from2, from3, from1, free0, free1;            // accumulators 2 -> 0, 3 -> 1, 1 -> 0; slots free again
+    __shared__ UnitInfo infos[2];
+    __shared__ int pos16[STAGES][4];                                  // first position of each 16 keys of a tile, -1: none
+    __shared__ float red_m[2][NT * 8], red_l[2][NT * 8];
     __shared__ uint32_t abort_word;
-    __shared__ float red_m[WARPS][16], red_l[WARPS][16];
     volatile uint32_t* abort_flag = &abort_word;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int split = blockIdx.x % a.n_splits, head = (blockIdx.x / a.n_splits) % a.n_kv_heads;
-    const int item = blockIdx.x / a.n_splits / a.n_kv_heads;
-    AttnItem it;
-    if (!attn_item(a, item, it)) return;
-    const int rows = it.n_tok * a.group;
-    const int pos_last = a.causal ? it.pos0 + it.n_tok - 1 : it.pos0;
-    const int seen_lo = a.window > 0 ? max(it.pos0 - a.window + 1, 0) : 0;     // positions some row of the item may see
-    int v_lo = 0, v_hi = 0;
-    if (a.list_mode == LIST_NONE) {
-        v_lo = (seen_lo & ~(TILE - 1)) + split * a.split_len;
-        v_hi = min(v_lo + a.split_len, pos_last + 1);
-    } else {
-        v_lo = split * a.split_len;
-        v_hi = min((split + 1) * a.split_len, a.s << a.page_shift);
-        const int hl = a.list_heads == 1 ? 0 : head;
-        const int32_t* src = a.lists + (static_cast<int64_t>(it.list) * a.list_heads + hl) * a.s;
-        for (int e = threadIdx.x; e < a.s; e += THREADS) {
-            const int id = src[e];
-            // a block all of whose positions are out of sight counts as not listed
-            list[e] = id >= 0 && id <= (pos_last >> a.page_shift) && pos_last >= 0 && ((id + 1) << a.page_shift) > seen_lo ? id : -1;
-        }
-    }
-    const int n_tiles = max(0, (v_hi - v_lo + TILE - 1) / TILE);
+    cudaTriggerProgrammaticLaunchCompletion();       // the join's blocks may take their places; they wait for this grid's end
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) { mbar_init(&full_bar[i], 1); mbar_init(&empty_bar[i], WARPS); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&unit_full[i], 1); mbar_init(&unit_empty[i], WARPS); }
+        mbar_init(&from1, 1); mbar_init(&from2, 1); mbar_init(&from3, 1); mbar_init(&free0, 1); mbar_init(&free1, 1);
         abort_word = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    __syncthreads();
 
-    // First position of virtual key v (a multiple of 16), or -1 where no block is listed.
-    auto pos_of = [&](int v) -> int {
-        if (a.list_mode == LIST_NONE) return v;
-        const int e = v >> a.page_shift;
-        if (e >= a.s || list[e] < 0) return -1;
-        return (list[e] << a.page_shift) + (v & (a.page_size - 1));
+    auto give_up = [&](uint32_t code) {
+        if (lane == 0) { dev_set_error(a.status, code); *abort_flag = 1; }
     };
 
-    float o[D / 8][4];
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
-
-    int issued = 0;                            // tiles whose copies were started
     if (warp == WARPS) {
         // ---------------- producer ----------------
-        if (lane == 0) {
-            const int box = a.box_rows, per_tile = TILE / box;
+        const int box = a.box_rows, per_tile = TILE / box, group_tiles = 32 / per_tile;
+        const int lane_tile = lane / per_tile, lane_box = lane % per_tile;
+        int tiles = 0, units = 0;                                     // pushed so far
+        bool ok = true, met = false;
+        Walk<TILE> walk;
+        Segment g;
+        walk.start(a);
+        while (ok && walk.next(a, g)) {
+            const AttnItem& it = g.it;
+            const int head = g.head, pos_last = it.pos_last, seen_lo = first_seen(a, it), n_tiles = g.t_hi - g.t_lo, rows = it.n_tok * a.group;
+            const int v_lo = g.v_base + g.t_lo * TILE, v_hi = min(v_lo + n_tiles * TILE, a.list_mode == LIST_NONE ? pos_last + 1 : a.s << a.page_shift);
             const int32_t* table = a.b.pages + it.seq * a.b.ld_pages;
-            for (int t = 0; t < n_tiles; ++t) {
-                const int st = t % STAGES;
-                if (t >= STAGES && !mbar_wait(&empty_bar[st], ((t / STAGES) - 1) & 1, abort_flag)) {
-                    dev_set_error(a.status, DEV_TIMEOUT_SMEM_EMPTY);
-                    *abort_flag = 1;
-                    break;
+            const int32_t* list = a.lists + (static_cast<int64_t>(it.list) * a.list_heads + (a.list_heads == 1 ? 0 : head)) * a.s;
+
+            // A lane per box: the lanes read the table entries of the next 32 boxes together, one group ahead of the copies,
+            // so that no copy waits for its page number.
+            auto entry = [&](int t, int& page, int& pos) {             // this lane's box of tile t + lane_tile
+                const int v = v_lo + (t + lane_tile) * TILE + lane_box * box;
+                page = pos = -1;
+                if (v >= v_hi) return;
+                if (a.list_mode == LIST_NONE) pos = v;
+                else {
+                    const int id = list[v >> a.page_shift];
+                    // a block all of whose positions are out of sight counts as not listed
+                    if (id >= 0 && pos_last >= 0 && id <= (pos_last >> a.page_shift) && ((id + 1) << a.page_shift) > seen_lo)
+                        pos = (id << a.page_shift) + (v & (a.page_size - 1));
                 }
-                unsigned char* dst = ring + st * stage_bytes<D>();
-                uint32_t bytes = 0;
-                int page[TILE / 16], row[TILE / 16];
+                if (pos < 0 || pos >= it.kv) { pos = -1; return; }
+                const int p = table[pos >> a.page_shift];
+                page = p < 0 || p >= a.n_pages ? a.n_pages : p;        // beyond the map: reads as zeros
+            };
+            int page, pos, next_page, next_pos;
+            entry(0, next_page, next_pos);
+            if (!met) __syncthreads();                                // the barriers exist; the first reads ran meanwhile
+            met = true;
+
+            const int ub = units & 1;
+            if (units >= 2 && !__all_sync(0xffffffffu, mbar_wait(&unit_empty[ub], ((units >> 1) - 1) & 1, abort_flag))) {
+                give_up(DEV_TIMEOUT_SMEM_EMPTY);
+                break;
+            }
+            if (lane == 0) {
+                infos[ub] = UnitInfo{rows, n_tiles, it.tok0, it.pos0, pos_last, it.kv, head, g.slot};
+                mbar_expect_tx(&unit_full[ub], static_cast<uint32_t>(rows) * D * 2);
+            }
+            __syncwarp();
+            if (lane < rows) {
+                const T* src = static_cast<const T*>(a.q) + static_cast<int64_t>(it.tok0 + lane / a.group) * a.ldq +
+                               static_cast<int64_t>(head * a.group + lane % a.group) * D;
+                bulk_load(ring + L::Q + (ub * NT * 8 + lane) * L::Q_PITCH, src, D * 2, &unit_full[ub]);
+            }
+            ++units;
+
+            for (int t0 = 0; t0 < n_tiles && ok; t0 += group_tiles) {
+                page = next_page;
+                pos = next_pos;
+                if (page == a.n_pages) dev_set_error(a.status, DEV_BAD_PAGE);
+                entry(t0 + group_tiles, next_page, next_pos);
+                for (int t = t0; t < min(n_tiles, t0 + group_tiles); ++t) {
+                    const int st = tiles % STAGES, round = tiles / STAGES;
+                    if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(&empty_bar[st], (round - 1) & 1, abort_flag))) {
+                        give_up(DEV_TIMEOUT_SMEM_EMPTY);
+                        ok = false;
+                        break;
+                    }
+                    const bool here = lane_tile == t - t0, mine = here && page >= 0;
+                    if (here)
+                        for (int x = 0; x < box / 16; ++x) {
+                            const int at = pos + 16 * x;               // whole 16-key units that no row can see are skipped
+                            pos16[st][lane_box * (box / 16) + x] = mine && at <= pos_last && at < it.kv ? at : -1;
+                        }
+                    const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, mine));
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (boxes) mbar_expect_tx(&full_bar[st], boxes * 2u * static_cast<uint32_t>(box) * D * 2);
+                        else mbar_arrive(&full_bar[st]);
+                    }
+                    ++tiles;
+                    __syncwarp();
+                    if (mine) {
+                        unsigned char* dst = ring + st * L::STAGE + lane_box * box * 128;
+                        const int row = pos & (a.page_size - 1);
 #pragma unroll
-                for (int u = 0; u < TILE / 16; ++u) {
-                    page[u] = -1;
-                    row[u] = 0;
-                    if (u >= per_tile) continue;
-                    const int v = v_lo + t * TILE + u * box, pos = v < v_hi ? pos_of(v) : -1;
-                    if (pos < 0 || pos >= it.kv) continue;
-                    const int p = table[pos >> a.page_shift];
-                    if (p < 0 || p >= a.n_pages) dev_set_error(a.status, DEV_BAD_PAGE);
-                    page[u] = p < 0 || p >= a.n_pages ? a.n_pages : p;     // beyond the map: reads as zeros
-                    row[u] = pos & (a.page_size - 1);
-                    bytes += 2u * static_cast<uint32_t>(box) * D * 2;
-                }
-                issued = t + 1;
-                if (bytes == 0) { mbar_arrive(&full_bar[st]); continue; }
-                mbar_expect_tx(&full_bar[st], bytes);
-#pragma unroll
-                for (int u = 0; u < TILE / 16; ++u) {
-                    if (page[u] < 0) continue;
-#pragma unroll
-                    for (int h = 0; h < D / 64; ++h) {
-                        tma_load_4d(dst + h * TILE * 128 + u * box * 128, maps.k, h * 64, row[u], head, page[u], &full_bar[st]);
-                        tma_load_4d(dst + TILE * D * 2 + h * TILE * 128 + u * box * 128, maps.v, h * 64, row[u], head, page[u], &full_bar[st]);
+                        for (int h = 0; h < D / 64; ++h) {
+                            tma_load_4d(dst + h * TILE * 128, maps.k, h * 64, row, head, page, &full_bar[st]);
+                            tma_load_4d(dst + TILE * D * 2 + h * TILE * 128, maps.v, h * 64, row, head, page, &full_bar[st]);
+                        }
                     }
                 }
             }
+        }
+        if (!met) __syncthreads();
+        if (lane == 0) walk.leave_cut(a);
+        const int ub = units & 1;
+        if (ok && units >= 2 && !__all_sync(0xffffffffu, mbar_wait(&unit_empty[ub], ((units >> 1) - 1) & 1, abort_flag)))
+            give_up(DEV_TIMEOUT_SMEM_EMPTY);
+        else if (ok && lane == 0) {
+            infos[ub].rows = 0;
+            mbar_arrive(&unit_full[ub]);
+        }
+        if (__any_sync(0xffffffffu, *abort_flag != 0) && lane == 0) {  // no copy may be in flight when the block leaves
+            for (int i = max(0, tiles - STAGES); i < tiles; ++i) mbar_wait(&full_bar[i % STAGES], (i / STAGES) & 1, nullptr);
+            for (int i = max(0, units - 2); i < units; ++i) mbar_wait(&unit_full[i & 1], (i >> 1) & 1, nullptr);
         }
     } else {
         // ---------------- compute ----------------
-        const int r0 = lane >> 2, c0 = (lane & 3) * 2;
-        uint32_t q[D / 16][4];
-        int qpos[2];
-        {
-            const T* base = static_cast<const T*>(a.q) + static_cast<int64_t>(head) * a.group * D;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int row = r0 + 8 * i;
-                const bool live = row < rows;
-                const int tok = live ? row / a.group : 0, g = live ? row % a.group : 0;
-                const T* src = base + static_cast<int64_t>(it.tok0 + tok) * a.ldq + g * D;
-                qpos[i] = live ? (a.causal ? it.pos0 + tok : it.pos0) : -1;
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    q[k][i] = live ? *reinterpret_cast<const uint32_t*>(src + k * 16 + c0) : 0u;
-                    q[k][2 + i] = live ? *reinterpret_cast<const uint32_t*>(src + k * 16 + 8 + c0) : 0u;
-                }
-            }
-        }
+        __syncthreads();
+        const int quad = lane & 3, r8 = lane >> 2;                    // this thread's query rows: 2 quad, 2 quad + 1 (+ 8 nt)
         const int mi = lane >> 3, mr = lane & 7;
-        const int k_row = warp * 16 + (mi >> 1) * 8 + mr, k_chunk = mi & 1;      // K: matrices (keys 0-7 | 8-15) x (d 0-7 | 8-15)
-        const int v_row = warp * 16 + (mi & 1) * 8 + mr, v_chunk = mi >> 1;      // V: the same with the roles swapped, transposed
-        bool ok = true;
-        for (int t = 0; t < n_tiles; ++t) {
-            const int st = t % STAGES;
-            ok = mbar_wait(&full_bar[st], (t / STAGES) & 1, abort_flag);
-            if (!__all_sync(0xffffffffu, ok)) {
-                ok = false;
-                if (lane == 0) { dev_set_error(a.status, DEV_TIMEOUT_TMA_FULL); *abort_flag = 1; }
+        const int k_row = warp * 16 + (mi & 1) * 8 + mr, k_chunk = mi >> 1;       // K as A: (keys 0-7 | 8-15) x (d 0-7), then d 8-15
+        const int v_row = warp * 16 + (mi >> 1) * 8 + mr, v_chunk = mi & 1;       // V^T as A: (d 0-7 | 8-15) x (keys 0-7), then 8-15
+        float* slot0 = reinterpret_cast<float*>(ring + L::SLOTS);
+        float* slot1 = reinterpret_cast<float*>(ring + L::SLOTS + L::SLOT);
+        int tiles = 0;
+        for (int units = 0;; ++units) {
+            const int ub = units & 1;
+            if (!__all_sync(0xffffffffu, mbar_wait(&unit_full[ub], (units >> 1) & 1, abort_flag))) {
+                give_up(DEV_TIMEOUT_TMA_FULL);
                 break;
             }
-            const int v = v_lo + t * TILE + warp * 16;
-            const int pos = v < v_hi ? pos_of(v) : -1;
-            if (pos >= 0 && pos <= pos_last) {
-                unsigned char* tile = ring + st * stage_bytes<D>();
-                const uint32_t ks = smem_u32(tile), vs = ks + TILE * D * 2;
-                if (pos + 16 > it.kv) {
-                    // values past the last position may hold anything: zero their rows
-                    const int first = max(it.kv - pos, 0);
-                    for (int x = lane; x < (16 - first) * (D / 64) * 8; x += 32) {
-                        const int rr = first + x / ((D / 64) * 8), c = x % ((D / 64) * 8);
-                        *reinterpret_cast<uint4*>(tile + TILE * D * 2 + (c >> 3) * TILE * 128 + (warp * 16 + rr) * 128 + (c & 7) * 16) =
-                            make_uint4(0, 0, 0, 0);
-                    }
-                    fence_async_smem();
-                    __syncwarp();
-                }
-                float sc[2][4] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+            const UnitInfo info = infos[ub];
+            if (info.rows == 0) break;
+            uint32_t q[NT][D / 16][2];
+            int qpos[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const unsigned char* src = ring + L::Q + (ub * NT * 8 + n * 8 + r8) * L::Q_PITCH + quad * 4;
+                const bool live = n * 8 + r8 < info.rows;
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
-                    uint32_t b[4];
-                    const int c = k * 2 + k_chunk;
-                    ldsm4(b, ks + (c >> 3) * TILE * 128 + k_row * 128 + (((c & 7) ^ (k_row & 7)) << 4));
-                    mma16816<T>(sc[0], q[k], b[0], b[1]);
-                    mma16816<T>(sc[1], q[k], b[2], b[3]);
+                    q[n][k][0] = live ? *reinterpret_cast<const uint32_t*>(src + k * 32) : 0u;
+                    q[n][k][1] = live ? *reinterpret_cast<const uint32_t*>(src + k * 32 + 16) : 0u;
                 }
-                const bool edge = pos + 15 > it.pos0 || (a.window > 0 && pos <= pos_last - a.window);
-                float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-                for (int n = 0; n < 2; ++n)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int i = j >> 1, kp = pos + n * 8 + c0 + (j & 1);
-                        sc[n][j] *= a.scale_log2;
-                        if (edge && (kp > qpos[i] || (a.window > 0 && kp <= qpos[i] - a.window))) sc[n][j] = -INFINITY;
-                        mx[i] = fmaxf(mx[i], sc[n][j]);
-                    }
-                float f[2], ref[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
-                    mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
-                    mx[i] = fmaxf(mx[i], m[i]);
-                    ref[i] = mx[i] == -INFINITY ? 0.0f : mx[i];
-                    f[i] = ex2(m[i] - ref[i]);
-                    m[i] = mx[i];
-                    l[i] *= f[i];
-                }
-                uint32_t p[4];
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        sc[n][j] = ex2(sc[n][j] - ref[j >> 1]);
-                        l[j >> 1] += sc[n][j];
-                    }
-                    p[2 * n] = Half2Of<T>::pack(sc[n][0], sc[n][1]);
-                    p[2 * n + 1] = Half2Of<T>::pack(sc[n][2], sc[n][3]);
-                }
-                if (__any_sync(0xffffffffu, f[0] != 1.0f || f[1] != 1.0f)) {
-#pragma unroll
-                    for (int i = 0; i < D / 8; ++i) { o[i][0] *= f[0]; o[i][1] *= f[0]; o[i][2] *= f[1]; o[i][3] *= f[1]; }
-                }
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    uint32_t b[4];
-                    const int c = k * 2 + v_chunk;
-                    ldsm4_t(b, vs + (c >> 3) * TILE * 128 + v_row * 128 + (((c & 7) ^ (v_row & 7)) << 4));
-                    mma16816<T>(o[2 * k], p, b[0], b[1]);
-                    mma16816<T>(o[2 * k + 1], p, b[2], b[3]);
+                    const int row = n * 8 + quad * 2 + i;
+                    qpos[n][i] = row >= info.rows ? -1 : a.causal ? info.pos0 + row / a.group : info.pos0;
                 }
             }
+            float o[NT][D / 16][4], m[NT][2], l[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                m[n][0] = m[n][1] = -INFINITY;
+                l[n][0] = l[n][1] = 0.0f;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[n][i][j] = 0.0f;
+            }
+            bool ok = true;
+            for (int t = 0; t < info.n_tiles; ++t, ++tiles) {
+                const int st = tiles % STAGES;
+                ok = __all_sync(0xffffffffu, mbar_wait(&full_bar[st], (tiles / STAGES) & 1, abort_flag));
+                if (!ok) break;
+                const int pos = pos16[st][warp];
+                if (pos >= 0) {
+                    unsigned char* tile = ring + st * L::STAGE;
+                    const uint32_t ks = smem_u32(tile), vs = ks + TILE * D * 2;
+                    if (pos + 16 > info.kv) {
+                        // values past the last position may hold anything: zero their rows
+                        const int first = info.kv - pos;
+                        for (int x = lane; x < (16 - first) * (D / 8); x += 32) {
+                            const int rr = first + x / (D / 8), c = x % (D / 8);
+                            *reinterpret_cast<uint4*>(tile + TILE * D * 2 + (c >> 3) * TILE * 128 + (warp * 16 + rr) * 128 + (c & 7) * 16) =
+                                make_uint4(0, 0, 0, 0);
+                        }
+                        fence_async_smem();
+                        __syncwarp();
+                    }
+                    float sc[NT][4];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) sc[n][j] = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        uint32_t x[4];
+                        const int c = k * 2 + k_chunk;
+                        ldsm4(x, ks + (c >> 3) * TILE * 128 + k_row * 128 + (((c & 7) ^ (k_row & 7)) << 4));
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma16816<T>(sc[n], x, q[n][k][0], q[n][k][1]);
+                    }
+                    const bool edge = pos + 15 > info.pos0 || (a.window > 0 && pos <= info.pos_last - a.window);
+                    bool grow = false;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int i = j & 1, kp = pos + r8 + (j >> 1) * 8;
+                            sc[n][j] *= a.scale_log2;
+                            if (edge && (kp > qpos[n][i] || (a.window > 0 && kp <= qpos[n][i] - a.window))) sc[n][j] = -INFINITY;
+                            grow |= sc[n][j] > m[n][i] + RESCALE_AT;
+                        }
+                    if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            float f[2];
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                float top = fmaxf(fmaxf(sc[n][i], sc[n][2 + i]), m[n][i]);
+                                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
+                                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+                                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+                                f[i] = m[n][i] == -INFINITY ? 0.0f : ex2(m[n][i] - top);
+                                m[n][i] = top;
+                                l[n][i] *= f[i];
+                            }
+#pragma unroll
+                            for (int k = 0; k < D / 16; ++k) {
+                                o[n][k][0] *= f[0]; o[n][k][1] *= f[1];
+                                o[n][k][2] *= f[0]; o[n][k][3] *= f[1];
+                            }
+                        }
+                    }
+                    uint32_t p[NT][2];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            sc[n][j] = ex2(sc[n][j] - (m[n][j & 1] == -INFINITY ? 0.0f : m[n][j & 1]));
+                            l[n][j & 1] += sc[n][j];
+                        }
+                        p[n][0] = transpose8(Half2Of<T>::pack(sc[n][0], sc[n][1]));
+                        p[n][1] = transpose8(Half2Of<T>::pack(sc[n][2], sc[n][3]));
+                    }
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        uint32_t x[4];
+                        const int c = k * 2 + v_chunk;
+                        ldsm4_t(x, vs + (c >> 3) * TILE * 128 + v_row * 128 + (((c & 7) ^ (v_row & 7)) << 4));
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma16816<T>(o[n][k], x, p[n][0], p[n][1]);
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&empty_bar[st]);
+            }
+            if (!ok) {
+                give_up(DEV_TIMEOUT_TMA_FULL);
+                break;
+            }
             __syncwarp();
-            if (lane == 0) mbar_arrive(&empty_bar[st]);
-        }
+            if (lane == 0) mbar_arrive(&unit_empty[ub]);              // its description and query rows have been read
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-            if ((lane & 3) == 0) { red_m[warp][r0 + 8 * i] = m[i]; red_l[warp][r0 + 8 * i] = l[i]; }
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int x = 4; x < 32; x <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], x);
+
+            // ---- the four accumulators: 2 -> 0 and 3 -> 1, then 1 -> 0 ----
+            auto at = [&](float* slot, int n, int k, int j) -> float& {
+                return slot[(n * 8 + quad * 2 + (j & 1)) * L::PITCH + k * 16 + (j >> 1) * 8 + r8];
+            };
+            auto put = [&](float* slot, int x, uint64_t* bar) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) at(slot, n, k, j) = o[n][k][j];
+                    if (r8 == 0)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) { red_m[x][n * 8 + quad * 2 + i] = m[n][i]; red_l[x][n * 8 + quad * 2 + i] = l[n][i]; }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar);
+            };
+            auto take = [&](float* slot, int x) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    float f[2], g[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float m2 = red_m[x][n * 8 + quad * 2 + i], top = fmaxf(m[n][i], m2), ref = top == -INFINITY ? 0.0f : top;
+                        f[i] = ex2(m[n][i] - ref);
+                        g[i] = ex2(m2 - ref);
+                        m[n][i] = top;
+                        l[n][i] = l[n][i] * f[i] + red_l[x][n * 8 + quad * 2 + i] * g[i];
+                    }
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) o[n][k][j] = o[n][k][j] * f[j & 1] + at(slot, n, k, j) * g[j & 1];
+                }
+                __syncwarp();
+            };
+            const uint32_t now = units & 1, before = (units - 1) & 1;
+            auto wait = [&](uint64_t* bar, uint32_t parity) {
+                ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+                if (!ok) give_up(DEV_TIMEOUT_ACC_FULL);
+                return ok;
+            };
+            if (warp == 2) {
+                if (units > 0 && !wait(&free0, before)) break;
+                put(slot0, 0, &from2);
+            } else if (warp == 3) {
+                if (units > 0 && !wait(&free1, before)) break;
+                put(slot1, 1, &from3);
+            } else if (warp == 1) {
+                if (!wait(&from3, now)) break;
+                take(slot1, 1);
+                put(slot1, 1, &from1);
+            } else {
+                if (!wait(&from2, now)) break;
+                take(slot0, 0);
+                if (!wait(&from1, now)) break;
+                take(slot1, 1);
+                if (lane == 0) mbar_arrive(&free1);
+                float inv[NT][2];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        inv[n][i] = l[n][i] == 0.0f ? 0.0f : 1.0f / l[n][i];
+                        const int row = n * 8 + quad * 2 + i;
+                        if (r8 == 0 && row < info.rows) {
+                            const int64_t out_row = static_cast<int64_t>(info.tok0 + row / a.group) * a.n_heads + info.head * a.group + row % a.group;
+                            const float lse2 = l[n][i] == 0.0f ? -INFINITY : m[n][i] + log2f(l[n][i]);
+                            if (info.slot >= 0) a.part_lse[info.slot * a.rows_cap + row] = lse2;
+                            else if (a.lse) a.lse[out_row] = lse2 / kLog2e;
+                        }
+                    }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) at(slot0, n, k, j) = l[n][j & 1] == 0.0f ? 0.0f : o[n][k][j] * inv[n][j & 1];
+                __syncwarp();
+                for (int x = lane; x < info.rows * (D / 4); x += 32) {
+                    const int row = x / (D / 4), c = x % (D / 4) * 4;
+                    const float4 y = *reinterpret_cast<const float4*>(slot0 + row * L::PITCH + c);
+                    const int tok = info.tok0 + row / a.group, h = info.head * a.group + row % a.group;
+                    if (info.slot >= 0) {
+                        *reinterpret_cast<float4*>(a.part_o + (static_cast<int64_t>(info.slot) * a.rows_cap + row) * D + c) = y;
+                    } else {
+                        T* dst = static_cast<T*>(a.out) + static_cast<int64_t>(tok) * a.ld_out + static_cast<int64_t>(h) * D + c;
+                        *reinterpret_cast<uint2*>(dst) = make_uint2(Half2Of<T>::pack(y.x, y.y), Half2Of<T>::pack(y.z, y.w));
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&free0);
+            }
         }
     }
-    // every copy has landed and been read (or waited for): the ring becomes the meeting place of the four accumulators
     __syncthreads();
-    if (*abort_flag) {
-        if (threadIdx.x == WARPS * 32)         // no copy may be in flight when the block leaves
-            for (int i = max(0, issued - STAGES); i < issued; ++i) mbar_wait(&full_bar[i % STAGES], (i / STAGES) & 1, nullptr);
-        __syncthreads();
-        return;
-    }
-    constexpr int PITCH = D + 4;
-    float* acc = reinterpret_cast<float*>(ring);                       // [WARPS][16][PITCH]
-    static_assert(WARPS * 16 * PITCH * 4 <= STAGES * stage_bytes<D>(), "the accumulators fit the ring");
-    if (warp < WARPS) {
-        const int r0 = lane >> 2, c0 = (lane & 3) * 2;
+}
+
+// Joins the pieces of the units that the shares cut: out = sum_i 2^(lse_i - max) o_i / sum_i 2^(lse_i - max). Block x takes the unit
+// that began in share x and was cut behind it, its rows divided over the y blocks. With a few rows and many pieces (one
+// sequence over the whole grid) a block takes one row and its four warps every fourth piece; with many rows and two or
+// three pieces each warp takes two rows. The launch overlaps the kernel before it (programmatic launch).
+template <class T, int D, bool MANY_ROWS>
+__global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttnArgs a)
+{
+    __shared__ float acc[MANY_ROWS ? 1 : 4][D], acc_l[4];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    cudaGridDependencySynchronize();
+    const Cut cut = reinterpret_cast<const Cut*>(a.cuts)[blockIdx.x];
+    const int c0 = blockIdx.x, c1 = cut.last, rows = cut.n_tok * a.group;
+    constexpr int N = D / 32;                    // consecutive values per lane
+    constexpr int ROWS = MANY_ROWS ? 8 : 1;
+    const int from = blockIdx.y * ROWS, to = min(rows, from + ROWS);
+    for (int row = from + (MANY_ROWS ? warp : 0); row < to; row += MANY_ROWS ? 4 : 1) {
+        auto slot = [&](int c) { return static_cast<int64_t>(2 * c + (c < c1 ? 1 : 0)) * a.rows_cap + row; };
+        float top = -INFINITY;
+        for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, a.part_lse[slot(c)]);
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-            *reinterpret_cast<float2*>(&acc[(warp * 16 + r0) * PITCH + i * 8 + c0]) = make_float2(o[i][0], o[i][1]);
-            *reinterpret_cast<float2*>(&acc[(warp * 16 + r0 + 8) * PITCH + i * 8 + c0]) = make_float2(o[i][2], o[i][3]);
-        }
-    }
-    __syncthreads();
-    constexpr int VEC = D / 4;
-    for (int x = threadIdx.x; x < rows * VEC; x += THREADS) {
-        const int row = x / VEC, c = (x % VEC) * 4;
-        float top = red_m[0][row];
-#pragma unroll
-        for (int w = 1; w < WARPS; ++w) top = fmaxf(top, red_m[w][row]);
+        for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
         const float ref = top == -INFINITY ? 0.0f : top;
-        float sum = 0.0f;
-        float4 y = make_float4(0, 0, 0, 0);
+        float y[N], sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) {
-            const float f = ex2(red_m[w][row] - ref);
-            sum += f * red_l[w][row];
-            const float4 z = *reinterpret_cast<const float4*>(&acc[(w * 16 + row) * PITCH + c]);
-            y.x += f * z.x; y.y += f * z.y; y.z += f * z.z; y.w += f * z.w;
+        for (int j = 0; j < N; ++j) y[j] = 0.0f;
+#pragma unroll 4
+        for (int c = c0 + (MANY_ROWS ? 0 : warp); c <= c1; c += MANY_ROWS ? 1 : 4) {
+            const int64_t s = slot(c);
+            const float f = ex2(a.part_lse[s] - ref);               // a piece that saw nothing holds zeros and -inf
+            sum += f;
+            const float* p = a.part_o + s * D + lane * N;
+            if constexpr (N == 4) {
+                const float4 z = *reinterpret_cast<const float4*>(p);
+                y[0] += f * z.x; y[1] += f * z.y; y[2] += f * z.z; y[3] += f * z.w;
+            } else {
+                const float2 z = *reinterpret_cast<const float2*>(p);
+                y[0] += f * z.x; y[1] += f * z.y;
+            }
+        }
+        if constexpr (!MANY_ROWS) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) acc[warp][lane * N + j] = y[j];
+            if (lane == 0) acc_l[warp] = sum;
+            __syncthreads();
+            sum = (acc_l[0] + acc_l[1]) + (acc_l[2] + acc_l[3]);
+#pragma unroll
+            for (int j = 0; j < N; ++j) y[j] = (acc[0][lane * N + j] + acc[1][lane * N + j]) + (acc[2][lane * N + j] + acc[3][lane * N + j]);
+            if (warp != 0) continue;
         }
         const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-        y.x *= inv; y.y *= inv; y.z *= inv; y.w *= inv;
-        const int tok = it.tok0 + row / a.group, h = head * a.group + row % a.group;
-        const int64_t out_row = static_cast<int64_t>(tok) * a.n_heads + h;
-        const float lse2 = sum == 0.0f ? -INFINITY : top + log2f(sum);
-        if (a.n_splits == 1) {
-            T* dst = static_cast<T*>(a.out) + static_cast<int64_t>(tok) * a.ld_out + h * D + c;
-            *reinterpret_cast<uint2*>(dst) = make_uint2(Half2Of<T>::pack(y.x, y.y), Half2Of<T>::pack(y.z, y.w));
-            if (c == 0 && a.lse) a.lse[out_row] = lse2 / kLog2e;
-        } else {
-            const int64_t part = static_cast<int64_t>(split) * a.b.T * a.n_heads + out_row;
-            if (sum != 0.0f) *reinterpret_cast<float4*>(a.part_o + part * D + c) = y;
-            if (c == 0) a.part_lse[part] = lse2;
-        }
+        const int64_t tok = cut.tok0 + row / a.group, h = cut.head * a.group + row % a.group;
+        T* dst = static_cast<T*>(a.out) + tok * a.ld_out + h * D + lane * N;
+#pragma unroll
+        for (int j = 0; j < N; j += 2) *reinterpret_cast<uint32_t*>(dst + j) = Half2Of<T>::pack(y[j] * inv, y[j + 1] * inv);
+        if (lane == 0 && a.lse) a.lse[tok * a.n_heads + h] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) / kLog2e;
     }
 }
 
-// Joins the splits of every row: weights 2^(lse_i - max). A warp per row.
-template <class T, int D>
-__global__ void __launch_bounds__(128) join_kernel(const AttnArgs a)
-{
-    cudaGridDependencySynchronize();
-    const int lane = threadIdx.x & 31;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5), rows = static_cast<int64_t>(a.b.T) * a.n_heads;
-    if (row >= rows) return;
-    float top = -INFINITY;
-    for (int i = lane; i < a.n_splits; i += 32) top = fmaxf(top, a.part_lse[i * rows + row]);
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-    constexpr int N = D / 32;                    // consecutive values per lane
-    float y[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) y[j] = 0.0f;
-    float sum = 0.0f;
-    const bool some = top > -INFINITY;
-    for (int i = 0; some && i < a.n_splits; ++i) {
-        const float part = a.part_lse[i * rows + row];
-        if (part == -INFINITY) continue;         // nothing was written there
-        const float f = ex2(part - top);
-        sum += f;
-        const float* src = a.part_o + (i * rows + row) * D + lane * N;
-        if constexpr (N == 4) {
-            const float4 z = *reinterpret_cast<const float4*>(src);
-            y[0] += f * z.x; y[1] += f * z.y; y[2] += f * z.z; y[3] += f * z.w;
-        } else {
-            const float2 z = *reinterpret_cast<const float2*>(src);
-            y[0] += f * z.x; y[1] += f * z.y;
-        }
-    }
-    const float inv = some ? 1.0f / sum : 0.0f;
-    const int64_t tok = row / a.n_heads, h = row % a.n_heads;
-    T* dst = static_cast<T*>(a.out) + tok * a.ld_out + h * D + lane * N;
-#pragma unroll
-    for (int j = 0; j < N; j += 2) *reinterpret_cast<uint32_t*>(dst + j) = Half2Of<T>::pack(y[j] * inv, y[j + 1] * inv);
-    if (lane == 0 && a.lse) a.lse[row] = some ? (top + log2f(sum)) / kLog2e : -INFINITY;
-}
-
-template <class T, int D>
+template <class T, int D, int NT>
 s3_status launch_split(const KvCacheState& c, const AttnArgs& a, cudaStream_t stream)
 {
+    using L = Layout<D, NT>;
     static bool raised[64] = {};                 // the attribute is kept per device; setting it twice does no harm
     int dev = 0;
     S3_CUDA_TRY(cudaGetDevice(&dev));
     if (dev >= 64 || !raised[dev]) {
-        S3_CUDA_TRY(cudaFuncSetAttribute(split_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<D>())));
+        S3_CUDA_TRY(cudaFuncSetAttribute(split_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::TOTAL));
         if (dev < 64) raised[dev] = true;
     }
     Maps maps;
     memcpy(maps.k, c.map_k, sizeof(maps.k));
     memcpy(maps.v, c.map_v, sizeof(maps.v));
-    const int64_t blocks = static_cast<int64_t>(a.n_items) * a.n_kv_heads * a.n_splits;
-    S3_REQUIRE(blocks < (int64_t(1) << 31), S3_ERR_UNSUPPORTED, "the batch needs too many thread blocks");
-    split_kernel<T, D><<<static_cast<unsigned>(blocks), THREADS, smem_bytes<D>(), stream>>>(maps, a);
+    split_kernel<T, D, NT><<<a.grid, THREADS, L::TOTAL, stream>>>(maps, a);
     S3_CUDA_TRY(cudaGetLastError());
     return S3_OK;
 }
 
 template <class T, int D>
-s3_status launch_join_typed(const AttnArgs& a, cudaStream_t stream)
+s3_status launch_rows(const KvCacheState& c, const AttnArgs& a, cudaStream_t stream)
 {
-    const int64_t rows = static_cast<int64_t>(a.b.T) * a.n_heads;
+    const int rows = (a.list_mode == LIST_PER_TOKEN ? 1 : a.b.max_q) * a.group;       // of the largest item
+    return rows <= 8 ? launch_split<T, D, 1>(c, a, stream) : launch_split<T, D, 2>(c, a, stream);
+}
+
+template <class T, int D>
+s3_status launch_join_typed(const AttnArgs& a, bool tile, cudaStream_t stream)
+{
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>((rows + 3) / 4));
+    const int most = min(a.rows_cap, (a.list_mode == LIST_PER_TOKEN ? 1 : min(a.b.max_q, a.rows_cap)) * a.group);     // rows of an item
+    cfg.gridDim = dim3(static_cast<unsigned>(a.grid - 1), static_cast<unsigned>(tile ? (most + 7) / 8 : most));
     cfg.blockDim = dim3(128);
     cfg.stream = stream;
     cudaLaunchAttribute attr;
@@ -393,7 +561,8 @@ s3_status launch_join_typed(const AttnArgs& a, cudaStream_t stream)
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    S3_CUDA_TRY(cudaLaunchKernelEx(&cfg, join_kernel<T, D>, a));
+    if (tile) S3_CUDA_TRY(cudaLaunchKernelEx(&cfg, join_kernel<T, D, true>, a));
+    else S3_CUDA_TRY(cudaLaunchKernelEx(&cfg, join_kernel<T, D, false>, a));
     return S3_OK;
 }
 
@@ -402,15 +571,15 @@ s3_status launch_join_typed(const AttnArgs& a, cudaStream_t stream)
 s3_status launch_attn_split(const KvCacheState& c, const AttnArgs& a, cudaStream_t stream)
 {
     const bool wide = c.d.head_dim == 128;
-    if (c.d.dtype == S3_BF16) return wide ? launch_split<__nv_bfloat16, 128>(c, a, stream) : launch_split<__nv_bfloat16, 64>(c, a, stream);
-    return wide ? launch_split<__half, 128>(c, a, stream) : launch_split<__half, 64>(c, a, stream);
+    if (c.d.dtype == S3_BF16) return wide ? launch_rows<__nv_bfloat16, 128>(c, a, stream) : launch_rows<__nv_bfloat16, 64>(c, a, stream);
+    return wide ? launch_rows<__half, 128>(c, a, stream) : launch_rows<__half, 64>(c, a, stream);
 }
 
-s3_status launch_attn_join(const KvCacheState& c, const AttnArgs& a, cudaStream_t stream)
+s3_status launch_attn_join(const KvCacheState& c, const AttnArgs& a, bool tile, cudaStream_t stream)
 {
     const bool wide = c.d.head_dim == 128;
-    if (c.d.dtype == S3_BF16) return wide ? launch_join_typed<__nv_bfloat16, 128>(a, stream) : launch_join_typed<__nv_bfloat16, 64>(a, stream);
-    return wide ? launch_join_typed<__half, 128>(a, stream) : launch_join_typed<__half, 64>(a, stream);
+    if (c.d.dtype == S3_BF16) return wide ? launch_join_typed<__nv_bfloat16, 128>(a, tile, stream) : launch_join_typed<__nv_bfloat16, 64>(a, tile, stream);
+    return wide ? launch_join_typed<__half, 128>(a, tile, stream) : launch_join_typed<__half, 64>(a, tile, stream);
 }
 
 }  // namespace s3

@@ -2,10 +2,11 @@
 //
 //   S = Q K^T (fp32, tensor memory);  P = 2^(scale log2e S - m);  O += P V;  out = O / sum P      one pass over the keys
 //
-// A thread block takes one (item, key head, split). The item's query rows (token, head of the group), packed, fill one or
-// two tiles of 128; keys come in tiles of 128.
-//   warp 0       TMA producer: Q once, then K and V tiles page by page into a ring of shared-memory slots (128-byte swizzle);
-//   warp 1       MMA issuer: one thread issues tcgen05.mma for S = Q K^T (both operands in shared memory) and O += P V (P read
+// A persistent thread block per SM walks its segments (a unit of one item and one key head, or a piece of it). The item's query
+// rows (token, head of the group), packed, fill one or two tiles of 128; keys come in tiles of 128.
+//   warp 0       TMA producer: finds the segments, copies Q, then K and V tiles page by page into a ring of shared-memory slots
+//                (128-byte swizzle), running ahead into the next segment;
+//   warp 1       MMA issuer: one elected lane issues tcgen05.mma for S = Q K^T (both operands in shared memory) and O += P V (P read
 //                from tensor memory, V as the MN-major operand, so no transpose is ever made);
 //   warp 2       zeroes the rows of a V tile that hold no position of the sequence (a page's tail may hold anything);
 //   warps 4-7, 8-11   two softmax groups, a thread per row: S from tensor memory into registers, running maximum, exponentials,
@@ -13,8 +14,8 @@
 // With two query tiles (PAIR) each group owns one and both use every key tile; with one query tile the groups take the even
 // and the odd key tiles, with an accumulator each, and are joined at the end. Either way one group's exponentials run while
 // the tensor core works for the other: the two sides need about the same time at head_dim 128.
-// O stays in tensor memory. It is rescaled only when a row's maximum grows by more than 2^8 over the reference its
-// exponentials use (P then stays below 2^8, well inside either type, and the sum in fp32); the MMA order makes S(j+1) complete
+// O stays in tensor memory. It is rescaled only when a row's maximum has grown far over the reference its exponentials use (P
+// stays below 2^14, inside either type, and the sum in fp32); the MMA order makes S(j+1) complete
 // only after O += P(j) V(j), so the group may touch O as soon as it sees the next S.
 //
 // Every mbarrier wait is bounded; one that runs out sets the status word and the block's abort flag, and the block waits for its
@@ -32,10 +33,17 @@ using namespace kv;
 constexpr int BM = 128, BN = 128;                  // query rows and keys per tile
 constexpr int THREADS = 384;
 constexpr int TMEM_COLS = 512;
-constexpr float RESCALE_AT = 8.0f;
+constexpr float RESCALE_AT = 8.0f;                 // a reference is moved to the row's maximum when that exceeds it by this,
+constexpr float CHECK_AT = 14.0f;                  // which is looked at when a weight may exceed 2^14
 
 struct Maps {
     alignas(64) unsigned char q[128], k[128], v[128];
+};
+
+// What the producer tells the other roles about a segment.
+struct SegInfo {
+    AttnItem it;
+    int head, t_lo, n_tiles, v_base, slot;         // n_tiles 0: no more segments
 };
 
 template <int D, bool PAIR>
@@ -43,37 +51,46 @@ struct Layout {
     static constexpr int TILE_BYTES = BN * D * 2;
     static constexpr int Q_TILES = PAIR ? 2 : 1;
     static constexpr int Q_BYTES = Q_TILES * BM * D * 2;
-    static constexpr int SLOTS = D == 128 ? 5 : 8;
+    static constexpr int SLOTS = (D == 128 ? 7 : 10) - Q_TILES;
     static constexpr int RING = Q_BYTES;
-    static constexpr int LIST = RING + SLOTS * TILE_BYTES;
-    static constexpr int BARS = LIST + S3_MAX_BLOCK_LIST * 4;
-    static constexpr int TOTAL = BARS + 256;
+    static constexpr int MEET = RING + SLOTS * TILE_BYTES;             // [2][128] floats: reference and sum of the odd tiles' group
+    static constexpr int BARS = MEET + 1024;
+    static constexpr int TOTAL = BARS + 512;
     static_assert(TOTAL <= 227 * 1024, "one thread block per SM");
 };
 
-__device__ __forceinline__ uint64_t desc_base(uint32_t saddr, uint32_t lbo, uint32_t sbo)
+// Shared-memory matrix descriptor, 128-byte swizzle: the low word holds the address and the leading offset, the high word the
+// stride between 8-row groups, the architecture's descriptor version and the swizzle.
+constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_lo(uint32_t saddr, uint32_t lbo) { return ((saddr >> 4) & 0x3FFFu) | ((lbo >> 4) << 16); }
+
+// The MMA warp issues as a whole, one elected lane doing the work: its addresses then are warp-uniform values, and an
+// instruction costs a few cycles to issue. (Behind `if (lane == 0)` each cost about 90, more than the 64 that a 128 x 128 x 16
+// product takes, and the two products of a tile needed 3900 cycles where 2048 will do.)
+__device__ __forceinline__ uint32_t elect_one()
 {
-    uint64_t d = 0;
-    d |= static_cast<uint64_t>((saddr >> 4) & 0x3FFFu);
-    d |= static_cast<uint64_t>(lbo >> 4) << 16;
-    d |= static_cast<uint64_t>(sbo >> 4) << 32;
-    d |= static_cast<uint64_t>(1) << 46;                 // descriptor version of this architecture
-    d |= static_cast<uint64_t>(2) << 61;                 // 128-byte swizzle
-    return d;
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p;
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool acc)
+__device__ __forceinline__ void mma_ss(uint32_t one, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool acc)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc ? 1u : 0u) : "memory");
+    asm volatile("{\n\t.reg .pred p, e;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %6, 0;\n\t"
+                 "mov.b64 da, {%1, %5};\n\tmov.b64 db, {%2, %5};\n\t"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc ? 1u : 0u),
+                 "r"(kDescHi), "r"(one) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool acc)
+__device__ __forceinline__ void mma_ts(uint32_t one, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool acc)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc ? 1u : 0u) : "memory");
+    asm volatile("{\n\t.reg .pred p, e;\n\t.reg .b64 db;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %6, 0;\n\t"
+                 "mov.b64 db, {%2, %5};\n\t"
+                 "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc ? 1u : 0u),
+                 "r"(kDescHi), "r"(one) : "memory");
 }
-__device__ __forceinline__ void commit(uint64_t* bar)
+__device__ __forceinline__ void commit(uint32_t one, uint64_t* bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+    asm volatile("{\n\t.reg .pred e;\n\tsetp.ne.b32 e, %1, 0;\n\t"
+                 "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(bar)), "r"(one) : "memory");
 }
 __device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -101,12 +118,101 @@ __device__ __forceinline__ void tm_st32(uint32_t taddr, const uint32_t (&u)[32])
         "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]), "r"(u[29]), "r"(u[30]), "r"(u[31]) : "memory");
 }
 
-__device__ __forceinline__ void tm_st32(uint32_t taddr, const float (&f)[32])
+__device__ __forceinline__ void tm_ld16(uint32_t taddr, float (&u)[16])
 {
-    uint32_t u[32];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=f"(u[0]), "=f"(u[1]), "=f"(u[2]), "=f"(u[3]), "=f"(u[4]), "=f"(u[5]), "=f"(u[6]), "=f"(u[7]),
+                   "=f"(u[8]), "=f"(u[9]), "=f"(u[10]), "=f"(u[11]), "=f"(u[12]), "=f"(u[13]), "=f"(u[14]), "=f"(u[15])
+                 : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tm_st16(uint32_t taddr, const float (&u)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+                 "f"(u[0]), "f"(u[1]), "f"(u[2]), "f"(u[3]), "f"(u[4]), "f"(u[5]), "f"(u[6]), "f"(u[7]),
+                 "f"(u[8]), "f"(u[9]), "f"(u[10]), "f"(u[11]), "f"(u[12]), "f"(u[13]), "f"(u[14]), "f"(u[15]) : "memory");
+}
+
+// ---- weights -------------------------------------------------------------------------------------
+typedef unsigned long long f32x2;
+
+__device__ __forceinline__ f32x2 pair_of(float a, float b)
+{
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void split_pair(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
+{
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)       // NaN if one is NaN
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float max_of(const float (&s)[32])
+{
+    float m[4];
 #pragma unroll
-    for (int i = 0; i < 32; ++i) u[i] = __float_as_uint(f[i]);
-    tm_st32(taddr, u);
+    for (int x = 0; x < 4; ++x) {
+        m[x] = max3(s[8 * x], s[8 * x + 1], s[8 * x + 2]);
+        m[x] = max3(m[x], s[8 * x + 3], s[8 * x + 4]);
+        m[x] = max3(m[x], s[8 * x + 5], s[8 * x + 6]);
+        m[x] = max3(m[x], s[8 * x + 7], s[8 * x + 7]);
+    }
+    return max3(max3(m[0], m[1], m[2]), m[3], m[3]);
+}
+// Weights 2^(s scale + ref) of 32 scores, packed to the type; their sum is added to `sum`. ex2 runs at 16 per clock and SM: 128 x 128
+// of them take the 1024 clocks that the tile's two products take. (Some of them by a polynomial on the multiply-add pipes
+// was tried: with the reduction, clamping and exponent steps it costs 12 clocks a pair and warp against 16, and gains nothing.)
+template <class T>
+__device__ __forceinline__ void weights(const float (&s)[32], f32x2 scale, f32x2 ref, uint32_t* p, f32x2 (&sum)[2])
+{
+#pragma unroll
+    for (int c = 0; c < 16; ++c) {
+        float x, y;
+        split_pair(fma2(pair_of(s[2 * c], s[2 * c + 1]), scale, ref), x, y);
+        x = ex2(x);
+        y = ex2(y);
+        sum[c & 1] = add2(sum[c & 1], pair_of(x, y));
+        p[c] = Half2Of<T>::pack(x, y);
+    }
+}
+__device__ __forceinline__ float total(const f32x2 (&sum)[2])
+{
+    float a, b;
+    split_pair(add2(sum[0], sum[1]), a, b);
+    return a + b;
+}
+
+// Eight lanes with eight 16-byte pieces each (lane r: pieces of row r) -> lane c has piece c of the eight rows, so that a store
+// instruction writes whole 128-byte lines of four rows instead of a piece of 32 (11 000 clocks per tile of fp32 results, 3000 so).
+__device__ __forceinline__ void transpose_pieces(uint32_t (&v)[8][4], int lane)
+{
+#pragma unroll
+    for (int bit = 1; bit < 8; bit <<= 1) {
+        const bool up = lane & bit;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (k & bit) continue;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t got = __shfl_xor_sync(0xffffffffu, up ? v[k][w] : v[k | bit][w], bit);
+                if (up) v[k][w] = got;
+                else v[k | bit][w] = got;
+            }
+        }
+    }
 }
 
 template <class T, int D, bool PAIR>
@@ -116,52 +222,44 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
     constexpr int SLOTS = L::SLOTS, AHEAD = PAIR ? 1 : 2;       // key tiles whose S is issued before the first P V
     extern __shared__ __align__(1024) unsigned char smem[];            // swizzled tiles start on 1024-byte boundaries
     unsigned char* ring = smem + L::RING;
-    int* list = reinterpret_cast<int*>(smem + L::LIST);
+    float* meet = reinterpret_cast<float*>(smem + L::MEET);
     uint64_t* full_bar = reinterpret_cast<uint64_t*>(smem + L::BARS);
     uint64_t* empty_bar = full_bar + SLOTS;
     uint64_t* s_full = empty_bar + SLOTS;
     uint64_t* p_full = s_full + 2;
-    uint64_t& q_full = p_full[2];
-    uint64_t& o_full = p_full[3];
-    uint64_t& dirty_bar = p_full[4];
-    uint64_t& clean_bar = p_full[5];
-    uint64_t& meet_bar = p_full[6];
-    uint32_t& tmem_slot = *reinterpret_cast<uint32_t*>(p_full + 7);
+    uint64_t* p_half = p_full + 2;
+    uint64_t* seg_full = p_half + 2;
+    uint64_t* seg_empty = seg_full + 2;
+    uint64_t& q_full = seg_empty[2];
+    uint64_t& q_empty = seg_empty[3];
+    uint64_t& o_full = seg_empty[4];
+    uint64_t& dirty_bar = seg_empty[5];
+    uint64_t& clean_bar = seg_empty[6];
+    uint64_t& meet_bar = seg_empty[7];
+    uint64_t& met_bar = seg_empty[8];
+    SegInfo* infos = reinterpret_cast<SegInfo*>(seg_empty + 9);
+    uint32_t& tmem_slot = *reinterpret_cast<uint32_t*>(infos + 2);
     volatile uint32_t* abort_flag = &tmem_slot + 1;
+    static_assert((2 * SLOTS + 19) * 8 + 2 * sizeof(SegInfo) + 8 <= 512, "barriers and descriptions fit");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int split = blockIdx.x % a.n_splits, head = (blockIdx.x / a.n_splits) % a.n_kv_heads;
-    const int item = blockIdx.x / a.n_splits / a.n_kv_heads;
-    AttnItem it;
-    if (!attn_item(a, item, it)) return;
-    const int tile_tok = min(BM / a.group, a.tok_per_item);            // tokens per 128-row tile
-    const int pos_last = a.causal ? it.pos0 + it.n_tok - 1 : it.pos0;
-    const int seen_lo = a.window > 0 ? max(it.pos0 - a.window + 1, 0) : 0;
-    int v_lo = 0, v_hi = 0;
-    if (a.list_mode == LIST_NONE) {
-        v_lo = (seen_lo & ~(BN - 1)) + split * a.split_len;
-        v_hi = min(v_lo + a.split_len, pos_last + 1);
-    } else {
-        v_lo = split * a.split_len;
-        v_hi = min((split + 1) * a.split_len, a.s << a.page_shift);
-        const int hl = a.list_heads == 1 ? 0 : head;
-        const int32_t* src = a.lists + (static_cast<int64_t>(it.list) * a.list_heads + hl) * a.s;
-        for (int e = threadIdx.x; e < a.s; e += THREADS) {
-            const int id = src[e];
-            // a block all of whose positions are out of sight counts as not listed
-            list[e] = id >= 0 && id <= (pos_last >> a.page_shift) && pos_last >= 0 && ((id + 1) << a.page_shift) > seen_lo ? id : -1;
-        }
-    }
-    const int n_tiles = max(0, (v_hi - v_lo + BN - 1) / BN);
-
+    cudaTriggerProgrammaticLaunchCompletion();       // the join's blocks may take their places; they wait for this grid's end
     if (threadIdx.x == 0) {
-        mbar_init(&q_full, 1);
         for (int i = 0; i < SLOTS; ++i) { mbar_init(&full_bar[i], 1); mbar_init(&empty_bar[i], 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_full[i], 128); }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s_full[i], 1);
+            mbar_init(&p_half[i], 4);                                  // the group's warps
+            mbar_init(&p_full[i], 4);
+            mbar_init(&seg_full[i], 1);
+            mbar_init(&seg_empty[i], 10);                              // MMA warp, cleaning warp, eight softmax warps
+        }
+        mbar_init(&q_full, 1);
+        mbar_init(&q_empty, 1);
         mbar_init(&o_full, 1);
         mbar_init(&dirty_bar, 1);
         mbar_init(&clean_bar, 1);
-        mbar_init(&meet_bar, 128);
+        mbar_init(&meet_bar, 4);
+        mbar_init(&met_bar, 4);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -172,187 +270,264 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = __reduce_max_sync(0xffffffffu, tmem_slot);   // the same in every lane, and known to be
     auto tm_s = [&](int i) { return tmem + 128 * i; };                 // scores, then weights, of group i
     auto tm_o = [&](int i) { return tmem + 256 + 128 * i; };           // its accumulator
+    const int tile_tok = min(BM / a.group, a.tok_per_item);            // tokens per 128-row tile
 
     // First position of virtual key v (a multiple of 16), or -1 where no block is listed.
-    auto pos_of = [&](int v) -> int {
+    auto pos_of = [&](const AttnItem& it, int head, int v) -> int {
         if (a.list_mode == LIST_NONE) return v;
         const int e = v >> a.page_shift;
-        if (e >= a.s || list[e] < 0) return -1;
-        return (list[e] << a.page_shift) + (v & (a.page_size - 1));
+        if (e >= a.s || it.pos_last < 0) return -1;
+        const int id = __ldg(a.lists + (static_cast<int64_t>(it.list) * a.list_heads + (a.list_heads == 1 ? 0 : head)) * a.s + e);
+        // a block all of whose positions are out of sight counts as not listed
+        if (id < 0 || id > (it.pos_last >> a.page_shift) || ((id + 1) << a.page_shift) <= first_seen(a, it)) return -1;
+        return (id << a.page_shift) + (v & (a.page_size - 1));
     };
-    // Whether a key tile has rows without a position of the sequence: their values have to be zeroed.
-    auto unclean = [&](int j) -> bool {
-        const int v0 = v_lo + j * BN;
+    // Whether the key tile at v0 has rows without a position of the sequence: their values have to be zeroed.
+    auto unclean = [&](const AttnItem& it, int head, int v0) -> bool {
         if (a.list_mode == LIST_NONE) return v0 + BN > it.kv;
         bool bad = false;
         for (int u = 0; u < BN; u += 16) {
-            const int pos = pos_of(v0 + u);
+            const int pos = pos_of(it, head, v0 + u);
             bad |= pos < 0 || pos + 16 > it.kv;
         }
         return bad;
     };
+    auto give_up = [&](uint32_t code) {
+        dev_set_error(a.status, code);
+        *abort_flag = 1;
+    };
 
-    // The launch gives every thread 168 registers; the four role warps hand theirs to the softmax rows (128 x 56 + 256 x 224 =
+    // The launch gives every thread 168 registers; the four role warps hand some of theirs to the softmax rows (128 x 104 + 256 x 200 =
     // 384 x 168).
-    int issued = 0;                                                    // ring loads started
+    uint32_t issued = 0;                                               // ring loads started
     if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (warp == 0) {
-        // ---------------- producer ----------------
-        if (lane == 0 && n_tiles > 0) {
-            mbar_expect_tx(&q_full, L::Q_TILES * static_cast<uint32_t>(tile_tok * a.group) * D * 2);
-            for (int i = 0; i < L::Q_TILES; ++i)
-                for (int h = 0; h < D / 64; ++h)
-                    tma_load_4d(smem + i * BM * D * 2 + h * BM * 128, maps.q, h * 64, 0, head, it.tok0 + i * tile_tok, &q_full);
-            const int32_t* table = a.b.pages + it.seq * a.b.ld_pages;
-            const int box = a.box_rows;
-            auto load = [&](int j, bool value) -> bool {
-                const int st = issued % SLOTS, round = issued / SLOTS;
-                if (round > 0 && !mbar_wait(&empty_bar[st], (round - 1) & 1, abort_flag)) {
-                    dev_set_error(a.status, DEV_TIMEOUT_SMEM_EMPTY);
-                    *abort_flag = 1;
-                    return false;
-                }
-                const void* map = value ? maps.v : maps.k;
-                unsigned char* dst = ring + st * L::TILE_BYTES;
-                // the count may run ahead of the copies: the barrier completes only with the arrival at the end
-                for (int u = 0; u < BN; u += box) {
-                    const int pos = pos_of(v_lo + j * BN + u);
-                    if (pos < 0 || pos >= it.kv) continue;
-                    int p = table[pos >> a.page_shift];
-                    if (p < 0 || p >= a.n_pages) {
-                        dev_set_error(a.status, DEV_BAD_PAGE);
-                        p = a.n_pages;                                 // beyond the map: reads as zeros
-                    }
-                    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(&full_bar[st])),
-                                 "r"(static_cast<uint32_t>(box) * D * 2) : "memory");
-#pragma unroll
-                    for (int h = 0; h < D / 64; ++h)
-                        tma_load_4d(dst + h * BN * 128 + u * 128, map, h * 64, pos & (a.page_size - 1), head, p, &full_bar[st]);
-                }
-                mbar_arrive(&full_bar[st]);
-                ++issued;
-                return true;
-            };
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+        if (warp == 0) {
+            // ---------------- producer ----------------
+            // A lane per box: the lanes read the table entries of the next 32 boxes together, a group of tiles ahead of the
+            // copies (one lane reading an entry before each copy bound the kernel at 2.5 us per key tile).
+            Walk<BN> walk;
+            Segment g, g_next;
+            walk.start(a);
+            bool some = walk.next(a, g), some_next = false;
+            const int box = a.box_rows, per_tile = BN / box, group_tiles = 32 / per_tile;
+            int segs = 0;
             bool ok = true;
-            for (int j = 0; j < min(AHEAD, n_tiles) && ok; ++j) ok = load(j, false);
-            for (int j = 0; j < n_tiles && ok; ++j) {
-                ok = load(j, true);
-                if (ok && j + AHEAD < n_tiles) ok = load(j + AHEAD, false);
-            }
-        }
-    } else if (warp == 1) {
-        // ---------------- MMA issuer ----------------
-        if (lane == 0 && n_tiles > 0) {
-            constexpr uint32_t fmt = sizeof(T) == 2 && Half2Of<T>::is_bf16 ? 1u : 0u;
-            constexpr uint32_t base = (1u << 4) | (fmt << 7) | (fmt << 10) | (static_cast<uint32_t>(BM >> 4) << 24);
-            constexpr uint32_t idesc_s = base | (static_cast<uint32_t>(BN >> 3) << 17);
-            constexpr uint32_t idesc_o = base | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17);     // V: MN-major
-            const uint32_t q_addr = smem_u32(smem), r_addr = smem_u32(ring);
-            uint32_t used = 0, cleaned = 0;
-            bool ok = true;
-            auto need = [&](uint64_t* bar, uint32_t parity, uint32_t code) {
-                if (ok && !mbar_wait(bar, parity, abort_flag)) {
-                    dev_set_error(a.status, code);
-                    *abort_flag = 1;
-                    ok = false;
-                }
+            auto wait = [&](uint64_t* bar, uint32_t parity) {
+                ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+                if (!ok && lane == 0) give_up(DEV_TIMEOUT_SMEM_EMPTY);
                 return ok;
             };
-            auto slot_ready = [&]() { return need(&full_bar[used % SLOTS], (used / SLOTS) & 1, DEV_TIMEOUT_TMA_FULL); };
-            auto scores = [&](int i, int qt, uint32_t st) {
-                tc_fence_after();
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    const uint32_t off = (k >> 2) * (BM * 128) + (k & 3) * 32;
-                    mma_ss(tm_s(i), desc_base(q_addr + qt * BM * D * 2 + off, 16, 1024), desc_base(r_addr + st * L::TILE_BYTES + off, 16, 1024),
-                           idesc_s, k > 0);
+            for (;;) {
+                if (segs >= 2 && !wait(&seg_empty[segs & 1], ((segs >> 1) - 1) & 1)) break;
+                if (lane == 0) {
+                    infos[segs & 1] = SegInfo{g.it, g.head, g.t_lo, some ? g.t_hi - g.t_lo : 0, g.v_base, g.slot};
+                    mbar_arrive(&seg_full[segs & 1]);
                 }
-                commit(&s_full[i]);
-            };
-            auto product = [&](int i, uint32_t st, bool acc) {
-                tc_fence_after();
-#pragma unroll
-                for (int k = 0; k < BN / 16; ++k)
-                    mma_ts(tm_o(i), tm_s(i) + k * 8, desc_base(r_addr + st * L::TILE_BYTES + k * 2048, BN * 128, 1024), idesc_o, acc || k > 0);
-            };
-            need(&q_full, 0, DEV_TIMEOUT_TMA_FULL);
-            for (int j = 0; j < min(AHEAD, n_tiles) && ok; ++j) {
-                if (!slot_ready()) break;
-                const uint32_t st = used % SLOTS;
-                if (PAIR) { scores(0, 0, st); scores(1, 1, st); }
-                else scores(j & 1, 0, st);
-                commit(&empty_bar[st]);
-                ++used;
-            }
-            for (int j = 0; j < n_tiles && ok; ++j) {
-                if (!slot_ready()) break;
-                const uint32_t sv = used % SLOTS;
-                ++used;
-                if (unclean(j)) {
-                    mbar_arrive(&dirty_bar);
-                    if (!need(&clean_bar, cleaned++ & 1, DEV_TIMEOUT_ACC_EMPTY)) break;
+                if (!some) break;
+                const int n_tiles = g.t_hi - g.t_lo, v_lo = g.v_base + g.t_lo * BN;
+                const int32_t* table = a.b.pages + g.it.seq * a.b.ld_pages;
+                auto entry = [&](int t, int& page, int& pos) {         // this lane's box of the group of tiles from t
+                    page = -1;
+                    pos = t + lane / per_tile < n_tiles ? pos_of(g.it, g.head, v_lo + t * BN + lane * box) : -1;
+                    if (pos < 0 || pos >= g.it.kv) return;
+                    const int p = __ldg(table + (pos >> a.page_shift));
+                    page = p < 0 || p >= a.n_pages ? a.n_pages : p;    // beyond the map: reads as zeros
+                    if (page == a.n_pages) dev_set_error(a.status, DEV_BAD_PAGE);
+                };
+                int t0 = 0, page0, pos0, page1, pos1;                  // groups from t0 and from t0 + group_tiles
+                entry(0, page0, pos0);
+                entry(group_tiles, page1, pos1);
+                if (segs > 0 && !wait(&q_empty, (segs - 1) & 1)) break;
+                ++segs;
+                if (lane == 0) {
+                    mbar_expect_tx(&q_full, L::Q_TILES * static_cast<uint32_t>(tile_tok * a.group) * D * 2);
+                    for (int i = 0; i < L::Q_TILES; ++i)
+                        for (int h = 0; h < D / 64; ++h)
+                            tma_load_4d(smem + i * BM * D * 2 + h * BM * 128, maps.q, h * 64, 0, g.head, g.it.tok0 + i * tile_tok, &q_full);
                 }
-                const bool more = j + AHEAD < n_tiles;
-                const uint32_t sk = used % SLOTS;
-                if (PAIR) {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        if (!need(&p_full[i], j & 1, DEV_TIMEOUT_ACC_EMPTY)) break;
-                        product(i, sv, j > 0);
-                        if (i == 1) commit(&empty_bar[sv]);
-                        if (more) {
-                            if (i == 0 && !slot_ready()) break;
-                            scores(i, i, sk);
-                        }
+                auto load = [&](int j, bool value) -> bool {
+                    const uint32_t st = issued % SLOTS, round = issued / SLOTS;
+                    const int x = j - t0, from = (x % group_tiles) * per_tile + lane % per_tile;
+                    const int pa = __shfl_sync(0xffffffffu, page0, from), pb = __shfl_sync(0xffffffffu, page1, from);
+                    const int qa = __shfl_sync(0xffffffffu, pos0, from), qb = __shfl_sync(0xffffffffu, pos1, from);
+                    const int page = x < group_tiles ? pa : pb, pos = x < group_tiles ? qa : qb;
+                    if (round > 0 && !wait(&empty_bar[st], (round - 1) & 1)) return false;
+                    const bool mine = lane < per_tile && page >= 0;
+                    const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, mine));
+                    if (lane == 0) {
+                        if (boxes) mbar_expect_tx(&full_bar[st], boxes * static_cast<uint32_t>(box) * D * 2);
+                        else mbar_arrive(&full_bar[st]);
                     }
-                    if (more && ok) { commit(&empty_bar[sk]); ++used; }
-                } else {
-                    const int i = j & 1;
-                    if (!need(&p_full[i], (j >> 1) & 1, DEV_TIMEOUT_ACC_EMPTY)) break;
-                    product(i, sv, j > 1);
-                    commit(&empty_bar[sv]);
-                    if (more) {
+                    ++issued;
+                    __syncwarp();
+                    if (mine) {
+                        unsigned char* dst = ring + st * L::TILE_BYTES + lane * box * 128;
+#pragma unroll
+                        for (int h = 0; h < D / 64; ++h)
+                            tma_load_4d(dst + h * BN * 128, value ? maps.v : maps.k, h * 64, pos & (a.page_size - 1), g.head, page, &full_bar[st]);
+                    }
+                    return true;
+                };
+                for (int j = 0; j < min(AHEAD, n_tiles) && ok; ++j) load(j, false);
+                for (int j = 0; j < n_tiles && ok; ++j) {
+                    if (!load(j, true)) break;
+                    if (j + AHEAD < n_tiles) load(j + AHEAD, false);
+                    // the next segment is looked up while the ring is full
+                    if (j == min(2, n_tiles - 1)) some_next = walk.next(a, g_next);
+                    if (j + 1 - t0 == group_tiles) {
+                        t0 += group_tiles;
+                        page0 = page1;
+                        pos0 = pos1;
+                        entry(t0 + group_tiles, page1, pos1);
+                    }
+                }
+                if (!ok) break;
+                g = g_next;
+                some = some_next;
+            }
+            if (lane == 0) walk.leave_cut(a);
+            if (lane == 0 && *abort_flag) {                            // no copy may be in flight when the block leaves
+                if (segs > 0) mbar_wait(&q_full, (segs - 1) & 1, nullptr);
+                for (uint32_t x = issued > SLOTS ? issued - SLOTS : 0; x < issued; ++x) mbar_wait(&full_bar[x % SLOTS], (x / SLOTS) & 1, nullptr);
+            }
+        } else if (warp == 1) {
+            // ---------------- MMA issuer ----------------
+            {
+                const uint32_t one = elect_one();
+                constexpr uint32_t fmt = Half2Of<T>::is_bf16 ? 1u : 0u;
+                constexpr uint32_t base = (1u << 4) | (fmt << 7) | (fmt << 10) | (static_cast<uint32_t>(BM >> 4) << 24);
+                constexpr uint32_t idesc_s = base | (static_cast<uint32_t>(BN >> 3) << 17);
+                constexpr uint32_t idesc_o = base | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17);     // V: MN-major
+                // 227 KB of shared memory: an address in 16-byte units never carries out of its 14 bits
+                const uint32_t q_desc = desc_lo(smem_u32(smem), 16), k_desc = desc_lo(smem_u32(ring), 16), v_desc = desc_lo(smem_u32(ring), BN * 128);
+                uint32_t used = 0, cleaned = 0, turns0 = 0, turns1 = 0;       // ring loads, cleaned tiles, weights taken from each group
+                bool ok = true;
+                auto need = [&](uint64_t* bar, uint32_t parity, uint32_t code) {
+                    ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+                    if (!ok && lane == 0) give_up(code);
+                    return ok;
+                };
+                auto slot_ready = [&]() { return need(&full_bar[used % SLOTS], (used / SLOTS) & 1, DEV_TIMEOUT_TMA_FULL); };
+                auto scores = [&](int i, int qt, uint32_t st) {
+                    tc_fence_after();
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k) {
+                        const uint32_t off = ((k >> 2) * (BM * 128) + (k & 3) * 32) >> 4;
+                        mma_ss(one, tm_s(i), q_desc + qt * (BM * D * 2 >> 4) + off, k_desc + st * (L::TILE_BYTES >> 4) + off, idesc_s, k > 0);
+                    }
+                    commit(one, &s_full[i]);
+                };
+                auto product = [&](int i, uint32_t st, bool acc, uint32_t parity) {
+#pragma unroll
+                    for (int k = 0; k < BN / 16; ++k) {
+                        if (k == 0 && !need(&p_half[i], parity, DEV_TIMEOUT_ACC_EMPTY)) return false;
+                        if (k == BN / 32 && !need(&p_full[i], parity, DEV_TIMEOUT_ACC_EMPTY)) return false;
+                        if (k % (BN / 32) == 0) tc_fence_after();
+                        mma_ts(one, tm_o(i), tm_s(i) + k * 8, v_desc + st * (L::TILE_BYTES >> 4) + k * (2048 >> 4), idesc_o, acc || k > 0);
+                    }
+                    return true;
+                };
+                for (int seg = 0; ok; ++seg) {
+                    if (!need(&seg_full[seg & 1], (seg >> 1) & 1, DEV_TIMEOUT_TMA_FULL)) break;
+                    const SegInfo& info = infos[seg & 1];              // stays there until this segment is done
+                    const int n_tiles = __reduce_max_sync(0xffffffffu, info.n_tiles), v_lo = __reduce_max_sync(0xffffffffu, info.v_base + info.t_lo * BN);
+                    if (n_tiles == 0) break;
+                    need(&q_full, seg & 1, DEV_TIMEOUT_TMA_FULL);
+                    for (int j = 0; j < min(AHEAD, n_tiles) && ok; ++j) {
                         if (!slot_ready()) break;
-                        scores(i, 0, sk);
-                        commit(&empty_bar[sk]);
+                        const uint32_t st = used % SLOTS;
+                        if (PAIR) { scores(0, 0, st); scores(1, 1, st); }
+                        else scores(j & 1, 0, st);
+                        commit(one, &empty_bar[st]);
                         ++used;
                     }
-                }
-            }
-            if (ok) commit(&o_full);
-        }
-    } else if (warp == 2) {
-        // ---------------- values past the sequence ----------------
-        // The MMA thread hands the tile over once it has landed. V tile j is ring load number 2j + AHEAD while key tiles still
-        // come (K_{j+AHEAD} follows V_j).
-        uint32_t at = min(AHEAD, n_tiles), handed = 0;
-        bool ok = true;
-        for (int j = 0; j < n_tiles && ok; ++j) {
-            if (unclean(j)) {
-                const uint32_t st = at % SLOTS;
-                ok = __all_sync(0xffffffffu, mbar_wait(&dirty_bar, handed++ & 1, abort_flag));
-                if (!ok) break;                                        // the MMA thread has reported why
-                for (int u = 0; u < BN; u += 16) {
-                    const int pos = pos_of(v_lo + j * BN + u);
-                    const int live = pos < 0 ? 0 : min(max(it.kv - pos, 0), 16);
-                    for (int x = lane; x < (16 - live) * (D / 8); x += 32) {
-                        const int row = u + live + x / (D / 8), c = x % (D / 8);
-                        *reinterpret_cast<uint4*>(ring + st * L::TILE_BYTES + (c >> 3) * BN * 128 + row * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    if (ok && n_tiles <= AHEAD) commit(one, &q_empty);
+                    for (int j = 0; j < n_tiles && ok; ++j) {
+                        if (!slot_ready()) break;
+                        const uint32_t sv = used % SLOTS;
+                        ++used;
+                        if (__any_sync(0xffffffffu, unclean(info.it, info.head, v_lo + j * BN))) {
+                            if (lane == 0) mbar_arrive(&dirty_bar);
+                            if (!need(&clean_bar, cleaned++ & 1, DEV_TIMEOUT_ACC_EMPTY)) break;
+                        }
+                        const bool more = j + AHEAD < n_tiles;
+                        const uint32_t sk = used % SLOTS;
+                        if (PAIR) {
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                if (!product(i, sv, j > 0, turns0 & 1)) break;
+                                if (i == 1) commit(one, &empty_bar[sv]);
+                                if (more) {
+                                    if (i == 0 && !slot_ready()) break;
+                                    scores(i, i, sk);
+                                }
+                            }
+                            ++turns0;
+                            if (more && ok) { commit(one, &empty_bar[sk]); ++used; }
+                        } else {
+                            const int i = j & 1;
+                            if (!product(i, sv, j > 1, (i ? turns1 : turns0) & 1)) break;
+                            if (i) ++turns1;
+                            else ++turns0;
+                            commit(one, &empty_bar[sv]);
+                            if (more) {
+                                if (!slot_ready()) break;
+                                scores(i, 0, sk);
+                                commit(one, &empty_bar[sk]);
+                                ++used;
+                            }
+                        }
+                        if (ok && more && j + AHEAD + 1 == n_tiles) commit(one, &q_empty);      // the segment's last S has been issued
                     }
+                    if (ok) commit(one, &o_full);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&seg_empty[seg & 1]);
                 }
-                fence_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&clean_bar);
             }
-            at += j + AHEAD < n_tiles ? 2 : 1;
+        } else if (warp == 2) {
+            // ---------------- values past the sequence ----------------
+            // The MMA thread hands a tile over once it has landed. V tile j of a segment is its ring load number 2j + AHEAD while
+            // key tiles still come (K_{j+AHEAD} follows V_j).
+            uint32_t at = 0, handed = 0;
+            SegInfo info;
+            for (int seg = 0;; ++seg) {
+                bool ok = __all_sync(0xffffffffu, mbar_wait(&seg_full[seg & 1], (seg >> 1) & 1, abort_flag));
+                if (!ok) break;                                        // another role has reported why
+                info = infos[seg & 1];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&seg_empty[seg & 1]);
+                if (info.n_tiles == 0) break;
+                at += min(AHEAD, info.n_tiles);
+                for (int j = 0; j < info.n_tiles && ok; ++j) {
+                    const int v0 = info.v_base + (info.t_lo + j) * BN;
+                    if (unclean(info.it, info.head, v0)) {
+                        const uint32_t st = at % SLOTS;
+                        ok = __all_sync(0xffffffffu, mbar_wait(&dirty_bar, handed++ & 1, abort_flag));
+                        if (!ok) break;
+                        for (int u = 0; u < BN; u += 16) {
+                            const int pos = pos_of(info.it, info.head, v0 + u);
+                            const int live = pos < 0 ? 0 : min(max(info.it.kv - pos, 0), 16);
+                            for (int x = lane; x < (16 - live) * (D / 8); x += 32) {
+                                const int row = u + live + x / (D / 8), c = x % (D / 8);
+                                *reinterpret_cast<uint4*>(ring + st * L::TILE_BYTES + (c >> 3) * BN * 128 + row * 128 + (c & 7) * 16) =
+                                    make_uint4(0, 0, 0, 0);
+                            }
+                        }
+                        fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&clean_bar);
+                    }
+                    at += j + AHEAD < info.n_tiles ? 2 : 1;
+                }
+                if (!ok) break;
+            }
         }
-    }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
         // ---------------- softmax ----------------
         const int i = (warp - 4) >> 2;                                 // group
         const int row = (warp & 3) * 32 + lane;                        // row of the tile = lane of tensor memory
@@ -360,179 +535,219 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
         const uint32_t my_s = tm_s(i) + lane_base, my_o = tm_o(i) + lane_base;
         const int first_tok = PAIR ? i * tile_tok : 0;                 // first token of the tile, relative to the item
         const int tok = first_tok + row / a.group, g = row % a.group;
-        const bool live = row < tile_tok * a.group && tok < it.n_tok;
-        const int qpos = a.causal ? it.pos0 + tok : it.pos0;
-        const int qlo = a.causal ? it.pos0 + first_tok : it.pos0;      // smallest and largest position of the tile's rows
-        const int qhi = a.causal ? min(qlo + tile_tok - 1, pos_last) : qlo;
-        float m = -INFINITY, l = 0.0f;                                 // reference of the exponentials (scaled, base 2), sum
+        const f32x2 scale2 = pair_of(a.scale_log2, a.scale_log2);
+        uint32_t turn = 0;                                             // key tiles this group has taken
         bool ok = true;
-        int turns = 0;
-        for (int j = PAIR ? 0 : i; j < n_tiles; j += PAIR ? 1 : 2, ++turns) {
-            ok = __all_sync(0xffffffffu, mbar_wait(&s_full[i], turns & 1, abort_flag));
-            if (!ok) {
-                if (lane == 0) { dev_set_error(a.status, DEV_TIMEOUT_ACC_FULL); *abort_flag = 1; }
-                break;
+        for (int seg = 0;; ++seg) {
+            ok = __all_sync(0xffffffffu, mbar_wait(&seg_full[seg & 1], (seg >> 1) & 1, abort_flag));
+            if (!ok) break;
+            const SegInfo& info = infos[seg & 1];                      // stays there until this segment is done
+            if (info.n_tiles == 0) break;
+            const bool live = row < tile_tok * a.group && tok < info.it.n_tok;
+            const int qpos = a.causal ? info.it.pos0 + tok : info.it.pos0;
+            const int qlo = a.causal ? info.it.pos0 + first_tok : info.it.pos0;      // smallest and largest position of the tile's rows
+            const int qhi = a.causal ? min(qlo + tile_tok - 1, info.it.pos_last) : qlo;
+            float m = -INFINITY, l = 0.0f;                             // reference of the exponentials (scaled, base 2), sum
+            int turns = 0;
+            for (int j = PAIR ? 0 : i; j < info.n_tiles; j += PAIR ? 1 : 2, ++turns, ++turn) {
+                const int v0 = info.v_base + (info.t_lo + j) * BN;
+                bool edge;                                             // some row may not see some key
+                if (a.list_mode == LIST_NONE) edge = v0 + BN - 1 > qlo || (a.window > 0 && v0 <= qhi - a.window);
+                else {
+                    edge = false;
+                    for (int u = 0; u < BN; u += 16) {
+                        const int pos = pos_of(info.it, info.head, v0 + u);
+                        edge |= pos < 0 || pos + 15 > qlo || (a.window > 0 && pos <= qhi - a.window);
+                    }
+                }
+                ok = __all_sync(0xffffffffu, mbar_wait(&s_full[i], turn & 1, abort_flag));
+                if (!ok) break;
+                tc_fence_after();
+                float s[4][32];
+                tm_ld32(my_s, s[0]);
+                wait_ld();
+#pragma unroll
+                for (int c = 1; c < 4; ++c) tm_ld32(my_s + 32 * c, s[c]);
+
+                // The weights are made with the reference as it stands. Before the first half of them is handed over, its sum and the
+                // largest score of the second half, which the multiply-add pipes find meanwhile, tell whether a weight may be too
+                // large (or a score is not a number); then, on the first tile and where keys are masked, the tile is done over
+                // with its maximum looked at first.
+                uint32_t p_lo[32], p_hi[32];
+                f32x2 sum[2] = {0, 0};                                 // pairs of +0
+                float ref = m == -INFINITY ? 0.0f : -m;
+                bool again = true;
+                if (!edge && turns > 0) {
+                    const f32x2 ref2 = pair_of(ref, ref);
+                    weights<T>(s[0], scale2, ref2, p_lo, sum);
+                    wait_ld();
+                    weights<T>(s[1], scale2, ref2, p_lo + 16, sum);
+                    const float a_hi = max_of(s[2]), b_hi = max_of(s[3]), top = max3(a_hi, b_hi, b_hi) * a.scale_log2;
+                    again = __any_sync(0xffffffffu, live && !(total(sum) <= 16384.0f && top <= m + CHECK_AT));
+                    if (!again) {
+                        tm_st32(my_s, p_lo);
+                        weights<T>(s[2], scale2, ref2, p_hi, sum);
+                        wait_st();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&p_half[i]);        // one arrival per warp: 128 on one barrier take turns
+                        weights<T>(s[3], scale2, ref2, p_hi + 16, sum);
+                        tm_st32(my_s + 32, p_hi);
+                    }
+                }
+                if (again) {
+                    wait_ld();
+                    if (edge) {
+#pragma unroll
+                        for (int u = 0; u < BN; u += 16) {
+                            const int pos = pos_of(info.it, info.head, v0 + u);
+                            const int hi = pos < 0 ? -1 : qpos - pos, lo = a.window > 0 ? hi - a.window : -1;      // visible: lo < c <= hi
+#pragma unroll
+                            for (int c = 0; c < 16; ++c)
+                                if (c > hi || c <= lo) s[u / 32][u % 32 + c] = -INFINITY;
+                        }
+                    }
+                    const float a_lo = max_of(s[0]), b_lo = max_of(s[1]), a_hi = max_of(s[2]), b_hi = max_of(s[3]);
+                    const float top = fmaxf(fmaxf(a_lo, b_lo), fmaxf(a_hi, b_hi)) * a.scale_log2;
+                    const bool grow = live && top > m + RESCALE_AT;
+                    if (__any_sync(0xffffffffu, grow)) {
+                        const float now = grow ? top : m;
+                        const float f = m == -INFINITY ? 0.0f : ex2(m - now);
+                        m = now;
+                        l *= f;
+                        if (turns > 0) {
+#pragma unroll
+                            for (int c = 0; c < D; c += 16) {          // narrow steps: the scores stay in registers meanwhile
+                                float o[16];
+                                tm_ld16(my_o + c, o);
+                                wait_ld();
+#pragma unroll
+                                for (int x = 0; x < 16; ++x) o[x] *= f;
+                                tm_st16(my_o + c, o);
+                            }
+                        }
+                    }
+                    ref = m == -INFINITY ? 0.0f : -m;
+                    const f32x2 ref2 = pair_of(ref, ref);
+                    sum[0] = sum[1] = 0;
+                    weights<T>(s[0], scale2, ref2, p_lo, sum);
+                    weights<T>(s[1], scale2, ref2, p_lo + 16, sum);
+                    tm_st32(my_s, p_lo);
+                    weights<T>(s[2], scale2, ref2, p_hi, sum);
+                    weights<T>(s[3], scale2, ref2, p_hi + 16, sum);
+                    tm_st32(my_s + 32, p_hi);
+                    // the first product of a segment overwrites the odd group's accumulator, which the even group may still be reading
+                    if (!PAIR && i == 1 && turns == 0 && seg > 0) {
+                        ok = __all_sync(0xffffffffu, mbar_wait(&met_bar, (seg - 1) & 1, abort_flag));
+                        if (!ok) break;
+                    }
+                }
+                wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (again) mbar_arrive(&p_half[i]);
+                    mbar_arrive(&p_full[i]);
+                }
+                l += total(sum);
             }
+            // ---------------- results ----------------
+            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&o_full, seg & 1, abort_flag));
+            if (ok && !PAIR) {
+                // the even tiles' group reads the odd one's accumulator itself (same lanes of tensor memory)
+                if (i == 1) {
+                    if (turns == 0 && seg > 0) ok = __all_sync(0xffffffffu, mbar_wait(&met_bar, (seg - 1) & 1, abort_flag));
+                    meet[row] = m;
+                    meet[128 + row] = l;
+                    __syncwarp();
+                    if (ok && lane == 0) mbar_arrive(&meet_bar);
+                } else ok = __all_sync(0xffffffffu, mbar_wait(&meet_bar, seg & 1, abort_flag));
+            }
+            if (!ok) break;
             tc_fence_after();
-            float s[4][32];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tm_ld32(my_s + 32 * c, s[c]);
-            wait_ld();
-            const int v0 = v_lo + j * BN;
-            bool edge;
-            if (a.list_mode == LIST_NONE) edge = v0 + BN - 1 > qlo || (a.window > 0 && v0 <= qhi - a.window);
-            else {
-                edge = false;
-                for (int u = 0; u < BN; u += 16) {
-                    const int pos = pos_of(v0 + u);
-                    edge |= pos < 0 || pos + 15 > qlo || (a.window > 0 && pos <= qhi - a.window);
+            if (PAIR || i == 0) {
+                float f_own = 1.0f, f_other = 0.0f;
+                if (!PAIR) {
+                    const float m1 = meet[row], l1 = meet[128 + row], both = fmaxf(m, m1), both_ref = both == -INFINITY ? 0.0f : both;
+                    f_own = ex2(m - both_ref);
+                    f_other = ex2(m1 - both_ref);
+                    l = l * f_own + l1 * f_other;
+                    m = both;
                 }
-            }
-            if (edge) {
-#pragma unroll
-                for (int u = 0; u < BN; u += 16) {
-                    const int pos = pos_of(v0 + u);
-                    const int hi = pos < 0 ? -1 : qpos - pos, lo = a.window > 0 ? hi - a.window : -1;      // visible: lo < c <= hi
-#pragma unroll
-                    for (int c = 0; c < 16; ++c)
-                        if (c > hi || c <= lo) s[u / 32][u % 32 + c] = -INFINITY;
+                const bool other = !PAIR && info.n_tiles > 1, empty = l == 0.0f;
+                const float inv = empty ? 0.0f : 1.0f / l;
+                f_own *= inv;
+                f_other *= inv;
+                const int t = info.it.tok0 + tok, h = info.head * a.group + g;
+                const int64_t out_row = static_cast<int64_t>(t) * a.n_heads + h;
+                const int64_t part = static_cast<int64_t>(info.slot) * a.rows_cap + first_tok * a.group + row;
+                const float lse2 = empty ? -INFINITY : m + log2f(l);
+                if (live) {
+                    if (info.slot >= 0) a.part_lse[part] = lse2;
+                    else if (a.lse) a.lse[out_row] = lse2 / kLog2e;
                 }
-            }
-            float mx[4] = {s[0][0], s[1][0], s[2][0], s[3][0]};
-#pragma unroll
-            for (int c = 1; c < 32; ++c)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) mx[x] = fmaxf(mx[x], s[x][c]);
-            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
-            const bool grow = live && top > m + RESCALE_AT;
-            if (__any_sync(0xffffffffu, grow)) {
-                const float now = live ? fmaxf(m, top) : m;
-                const float f = m == -INFINITY ? 0.0f : ex2(m - now);
-                m = now;
-                l *= f;
-                if (turns > 0) {
-#pragma unroll
-                    for (int c = 0; c < D; c += 32) {
-                        float o[32];
-                        tm_ld32(my_o + c, o);
-                        wait_ld();
-#pragma unroll
-                        for (int x = 0; x < 32; ++x) o[x] *= f;
-                        tm_st32(my_o + c, o);
-                    }
-                }
-            }
-            const float ref = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                uint32_t p[32];
-#pragma unroll
-                for (int c = 0; c < 32; ++c) {
-                    float &x = s[2 * half + c / 16][(2 * c) % 32], &y = s[2 * half + c / 16][(2 * c) % 32 + 1];
-                    x = ex2(fmaf(x, a.scale_log2, -ref));
-                    y = ex2(fmaf(y, a.scale_log2, -ref));
-                    p[c] = Half2Of<T>::pack(x, y);
-                }
-                tm_st32(my_s + 32 * half, p);
-            }
-            wait_st();
-            tc_fence_before();
-            mbar_arrive(&p_full[i]);
-            float sum[4] = {0, 0, 0, 0};
-#pragma unroll
-            for (int c = 0; c < 32; ++c)
-#pragma unroll
-                for (int x = 0; x < 4; ++x) sum[x] += s[x][c];
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        }
-        // ---------------- results ----------------
-        if (ok && n_tiles > 0) {
-            ok = __all_sync(0xffffffffu, mbar_wait(&o_full, 0, abort_flag));
-            if (!ok && lane == 0) { dev_set_error(a.status, DEV_TIMEOUT_ACC_FULL); *abort_flag = 1; }
-        }
-        tc_fence_after();
-        float f_own = 1.0f;
-        float* meet = reinterpret_cast<float*>(ring);                  // [2][128] then [128][D + 4]: the odd tiles' share
-        constexpr int PITCH = D + 4;
-        if (!PAIR && ok) {
-            // every copy has landed and every MMA has read its operands: the ring is free
-            if (i == 1) {
-                meet[row] = m;
-                meet[128 + row] = l;
-                if (turns > 0) {
-#pragma unroll
-                    for (int c = 0; c < D; c += 32) {
-                        float o[32];
-                        tm_ld32(my_o + c, o);
-                        wait_ld();
-#pragma unroll
-                        for (int x = 0; x < 32; x += 4)
-                            *reinterpret_cast<float4*>(meet + 256 + row * PITCH + c + x) = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
-                    }
-                }
-            }
-            if (i == 1) mbar_arrive(&meet_bar);
-            else {
-                ok = __all_sync(0xffffffffu, mbar_wait(&meet_bar, 0, abort_flag));
-                if (!ok && lane == 0) { dev_set_error(a.status, DEV_TIMEOUT_ACC_FULL); *abort_flag = 1; }
-            }
-        }
-        if (ok && (PAIR || i == 0)) {
-            float f_other = 0.0f;
-            if (!PAIR) {
-                const float m1 = meet[row], l1 = meet[128 + row], both = fmaxf(m, m1), ref = both == -INFINITY ? 0.0f : both;
-                f_own = ex2(m - ref);
-                f_other = ex2(m1 - ref);
-                l = l * f_own + l1 * f_other;
-                m = both;
-            }
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-            const int t = it.tok0 + tok, h = head * a.group + g;
-            const int64_t out_row = static_cast<int64_t>(t) * a.n_heads + h;
-            const int64_t part = static_cast<int64_t>(split) * a.b.T * a.n_heads + out_row;
-            const float lse2 = l == 0.0f ? -INFINITY : m + log2f(l);
-            if (live) {
-                if (a.n_splits > 1) a.part_lse[part] = lse2;
-                else if (a.lse) a.lse[out_row] = lse2 / kLog2e;
-            }
-#pragma unroll
-            for (int c = 0; c < D; c += 32) {
-                float o[32];
-                if (turns > 0) {
+                // a store's lane writes piece lane % 8 of the lines of rows x + 8 (lane / 8)
+                auto scaled = [&](int c, float (&o)[32]) {             // 32 results of this lane's row
                     tm_ld32(my_o + c, o);
                     wait_ld();
-                }
-                const bool other = !PAIR && n_tiles > 1;
 #pragma unroll
-                for (int x = 0; x < 32; x += 4) {
-                    float4 z = make_float4(0, 0, 0, 0);
-                    if (other) z = *reinterpret_cast<const float4*>(meet + 256 + row * PITCH + c + x);
-                    o[x] = turns == 0 || l == 0.0f ? 0.0f : (o[x] * f_own + z.x * f_other) * inv;
-                    o[x + 1] = turns == 0 || l == 0.0f ? 0.0f : (o[x + 1] * f_own + z.y * f_other) * inv;
-                    o[x + 2] = turns == 0 || l == 0.0f ? 0.0f : (o[x + 2] * f_own + z.z * f_other) * inv;
-                    o[x + 3] = turns == 0 || l == 0.0f ? 0.0f : (o[x + 3] * f_own + z.w * f_other) * inv;
-                }
-                if (!live) continue;
-                if (a.n_splits > 1) {
-                    if (l != 0.0f)
+                    for (int x = 0; x < 32; ++x) o[x] = empty ? 0.0f : o[x] * f_own;
+                    if (other) {
+                        float z[32];
+                        tm_ld32(tm_o(1) + lane_base + c, z);
+                        wait_ld();
 #pragma unroll
-                        for (int x = 0; x < 32; x += 4)
-                            *reinterpret_cast<float4*>(a.part_o + part * D + c + x) = make_float4(o[x], o[x + 1], o[x + 2], o[x + 3]);
+                        for (int x = 0; x < 32; ++x) o[x] = empty ? 0.0f : fmaf(z[x], f_other, o[x]);
+                    }
+                };
+                const uint32_t alive = __ballot_sync(0xffffffffu, live);
+                const int my_piece = lane & 7, my_row = lane & 24;
+                if (info.slot >= 0) {
+                    float* base = a.part_o + (part - lane) * D;        // the warp's first row
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 32) {
+                        float o[32];
+                        scaled(c, o);
+                        uint32_t v[8][4];
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) v[x / 4][x % 4] = __float_as_uint(o[x]);
+                        transpose_pieces(v, lane);
+#pragma unroll
+                        for (int x = 0; x < 8; ++x)
+                            if (alive >> (my_row + x) & 1)
+                                *reinterpret_cast<uint4*>(base + (my_row + x) * D + c + my_piece * 4) = make_uint4(v[x][0], v[x][1], v[x][2], v[x][3]);
+                    }
                 } else {
-                    T* dst = static_cast<T*>(a.out) + static_cast<int64_t>(t) * a.ld_out + h * D + c;
+                    T* dst = static_cast<T*>(a.out) + static_cast<int64_t>(t) * a.ld_out + static_cast<int64_t>(h) * D;
+                    const uint64_t mine = reinterpret_cast<uint64_t>(dst);
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 64) {
+                        uint32_t v[8][4];
 #pragma unroll
-                    for (int x = 0; x < 32; x += 8)
-                        *reinterpret_cast<uint4*>(dst + x) = make_uint4(Half2Of<T>::pack(o[x], o[x + 1]), Half2Of<T>::pack(o[x + 2], o[x + 3]),
-                                                                        Half2Of<T>::pack(o[x + 4], o[x + 5]), Half2Of<T>::pack(o[x + 6], o[x + 7]));
+                        for (int y = 0; y < 2; ++y) {
+                            float o[32];
+                            scaled(c + 32 * y, o);
+#pragma unroll
+                            for (int x = 0; x < 32; x += 2) v[4 * y + x / 8][x / 2 % 4] = Half2Of<T>::pack(o[x], o[x + 1]);
+                        }
+                        transpose_pieces(v, lane);
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) {
+                            T* to = reinterpret_cast<T*>(__shfl_sync(0xffffffffu, mine, my_row + x));
+                            if (alive >> (my_row + x) & 1)
+                                *reinterpret_cast<uint4*>(to + c + my_piece * 8) = make_uint4(v[x][0], v[x][1], v[x][2], v[x][3]);
+                        }
+                    }
                 }
+                tc_fence_before();
+                __syncwarp();
+                if (!PAIR && lane == 0) mbar_arrive(&met_bar);
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&seg_empty[seg & 1]);
         }
+        if (!ok && lane == 0) give_up(DEV_TIMEOUT_ACC_FULL);
         tc_fence_before();
-    }
-    __syncthreads();
-    if (*abort_flag && threadIdx.x == 0) {                             // no copy may be in flight when the block leaves
-        if (n_tiles > 0) mbar_wait(&q_full, 0, nullptr);
-        for (int x = max(0, issued - SLOTS); x < issued; ++x) mbar_wait(&full_bar[x % SLOTS], (x / SLOTS) & 1, nullptr);
     }
     __syncthreads();
     if (warp == 1) {
@@ -558,9 +773,7 @@ s3_status launch_tile(const KvCacheState& c, const AttnArgs& a, cudaStream_t str
     const int tile_tok = BM / a.group < a.tok_per_item ? BM / a.group : a.tok_per_item;
     s3_status st = make_kv_query_map(maps.q, c, a.q, a.ldq, a.b.T, a.group, tile_tok);
     if (st != S3_OK) return st;
-    const int64_t blocks = static_cast<int64_t>(a.n_items) * a.n_kv_heads * a.n_splits;
-    S3_REQUIRE(blocks < (int64_t(1) << 31), S3_ERR_UNSUPPORTED, "the batch needs too many thread blocks");
-    tile_kernel<T, D, PAIR><<<static_cast<unsigned>(blocks), THREADS, L::TOTAL, stream>>>(maps, a);
+    tile_kernel<T, D, PAIR><<<a.grid, THREADS, L::TOTAL, stream>>>(maps, a);
     S3_CUDA_TRY(cudaGetLastError());
     return S3_OK;
 }

@@ -85,14 +85,23 @@ __device__ __forceinline__ int seq_of_row(const KvBatchDev& b, int t)
 
 enum { LIST_NONE = 0, LIST_PER_TOKEN = 1, LIST_PER_SEQ = 2 };
 
-// Launch parameters of the attention kernels. A thread block takes one (item, key head, split): an item is a run of
-// tok_per_item new tokens of one sequence (with lists per token: one token), its query rows (token, head of the group)
-// packed token by token; a split is a range of split_len virtual keys, counted from the first tile that the item sees. Virtual key v of an item is position
-// block(v / page_size) * page_size + v % page_size, block(e) = e for the whole cache and = list[e] for a list.
+// Launch parameters of the attention kernels.
+//
+// An item is a run of tok_per_item new tokens of one sequence (with lists per token: one token); its query rows under one key
+// head, (token, head of the group) packed token by token, are worked on together. Keys are counted virtually: virtual key v is
+// position block(v / page_size) * page_size + v % page_size, block(e) = e for the whole cache and = list[e] for a list, and
+// are taken in tiles from the first one that some row of the item sees.
+//
+// The grid's thread blocks share the work in one of two ways, which the host chooses:
+//   share = 0   unit u = (item, key head), whole, goes to block u mod grid;
+//   share > 0   the tiles of all units, laid end to end (key head by key head, item by item), are cut into equal shares of `share`
+//               tiles or less, one per block, whatever the lengths are. A unit that a cut divides is worked on in pieces; a
+//               piece's result goes to a slot of its block (each has at most two pieces: one that began before its share and
+//               one that ends after it) and the join kernel adds the pieces up.
 struct AttnArgs {
     KvBatchDev b;
     int32_t n_heads, n_kv_heads, group, page_size, page_shift, box_rows, n_pages, head_dim;
-    float scale, scale_log2;
+    float scale_log2;
     int32_t causal, window;
     const int32_t* lists;
     int32_t s, list_heads, list_mode;
@@ -101,46 +110,248 @@ struct AttnArgs {
     void* out;
     int64_t ld_out;
     float* lse;
-    float* part_o;              // [n_splits][T * n_heads][head_dim]
-    float* part_lse;            // [n_splits][T * n_heads], base 2
-    int32_t n_splits, split_len, tok_per_item, n_items, one_item_per_seq;
+    float* part_o;              // [2 * grid][rows_cap][head_dim]
+    float* part_lse;            // [2 * grid][rows_cap], base 2
+    int32_t* cuts;              // [grid][8]: the unit that the cut behind a block's share divides first, see Cut
+    int32_t grid, share_min, rows_cap, tok_per_item, n_items, one_item_per_seq;
     uint32_t* status;
 };
 
 struct AttnItem {
     int seq, tok0, n_tok;       // first packed row, rows
-    int pos0, kv;               // position of the first row, cached positions
+    int pos0, pos_last, kv;     // positions of the first and last row, cached positions
     int list;                   // row of the lists
 };
 
+__device__ __forceinline__ AttnItem make_item(const AttnArgs& a, int seq, const SeqSpan& s, int idx)
+{
+    AttnItem it;
+    it.seq = seq;
+    it.tok0 = s.q0 + idx * a.tok_per_item;
+    it.n_tok = max(min(a.tok_per_item, s.n - idx * a.tok_per_item), 0);
+    it.kv = s.kv;
+    it.pos0 = a.causal ? s.kv - s.n + idx * a.tok_per_item : s.kv - 1;
+    it.pos_last = a.causal ? it.pos0 + it.n_tok - 1 : it.pos0;
+    it.list = a.list_mode == LIST_PER_TOKEN ? it.tok0 : seq;
+    return it;
+}
+
+// First position that some row of the item may see.
+__device__ __forceinline__ int first_seen(const AttnArgs& a, const AttnItem& it)
+{
+    return a.window > 0 ? max(it.pos0 - a.window + 1, 0) : 0;
+}
+
+// Key tiles of an item, at least one (rows that see nothing still have a result to write).
+template <int TILE>
+__device__ __forceinline__ int item_tiles(const AttnArgs& a, const AttnItem& it)
+{
+    const int keys = a.list_mode == LIST_NONE ? it.pos_last + 1 - (first_seen(a, it) & ~(TILE - 1)) : a.s << a.page_shift;
+    return max((keys + TILE - 1) / TILE, 1);
+}
+
+__device__ __forceinline__ int seq_items(const AttnArgs& a, const SeqSpan& s)
+{
+    return (s.n + a.tok_per_item - 1) / a.tok_per_item;
+}
+
+// Item number -> item; a whole warp. False when there is no such item.
 __device__ __forceinline__ bool attn_item(const AttnArgs& a, int item, AttnItem& it)
 {
+    int seq = item, idx = 0;
     if (a.list_mode == LIST_PER_TOKEN) {
-        it.seq = seq_of_row(a.b, item);
-        const SeqSpan s = load_seq(a.b, it.seq, a.status);
-        it.tok0 = item;
-        it.n_tok = item < s.q0 + s.n ? 1 : 0;
-        it.kv = s.kv;
-        it.pos0 = s.kv - s.n + (item - s.q0);
-        it.list = item;
-    } else {
-        int idx = 0;
-        if (a.one_item_per_seq) it.seq = item;
-        else {
-            const KvBatchDev& b = a.b;
-            const int per = a.tok_per_item;
-            if (!locate_item(b.n_seqs, item, [&](int i) { return (load_seq(b, i, nullptr).n + per - 1) / per; }, it.seq, idx)) return false;
-        }
-        const SeqSpan s = load_seq(a.b, it.seq, a.status);
-        it.tok0 = s.q0 + idx * a.tok_per_item;
-        it.n_tok = min(a.tok_per_item, s.n - idx * a.tok_per_item);
-        it.kv = s.kv;
-        it.pos0 = s.kv - s.n + idx * a.tok_per_item;
-        it.list = it.seq;
+        seq = seq_of_row(a.b, item);
+        const SeqSpan s = load_seq(a.b, seq, a.status);
+        if (item < s.q0 || item >= s.q0 + s.n) return false;
+        it = make_item(a, seq, s, item - s.q0);
+        return true;
     }
-    if (!a.causal) it.pos0 = it.kv - 1;
+    if (!a.one_item_per_seq &&
+        !locate_item(a.b.n_seqs, item, [&](int i) { return seq_items(a, load_seq(a.b, i, nullptr)); }, seq, idx)) return false;
+    it = make_item(a, seq, load_seq(a.b, seq, a.status), idx);
     return it.n_tok > 0;
 }
+
+// sum of floor((a i + b) / m) for i in [0, n), with a n + b < 2^32, m > 0. Each step takes out the whole parts and swaps the roles of
+// the two axes of the lattice, as in Euclid's algorithm.
+__device__ __forceinline__ int64_t floor_sum(uint32_t n, uint32_t m, uint32_t a, uint32_t b)
+{
+    int64_t sum = 0;
+    for (;;) {
+        const uint32_t qa = a / m, qb = b / m;
+        sum += static_cast<int64_t>(n) * (n - 1) / 2 * qa + static_cast<int64_t>(n) * qb;
+        a -= qa * m;
+        b -= qb * m;
+        const uint32_t top = a * n + b;
+        if (top < m) return sum;
+        n = top / m;
+        b = top - n * m;
+        const uint32_t t = a;
+        a = m;
+        m = t;
+    }
+}
+
+// Tiles of one key head over the items of sequence i.
+template <int TILE>
+__device__ __forceinline__ int64_t seq_tiles(const AttnArgs& a, int i)
+{
+    const SeqSpan s = load_seq(a.b, i, nullptr);
+    const int items = seq_items(a, s);
+    if (items == 0) return 0;
+    const int last = item_tiles<TILE>(a, make_item(a, i, s, items - 1));
+    if (items == 1) return last;
+    if (a.list_mode != LIST_NONE || !a.causal) return static_cast<int64_t>(items) * last;
+    if (a.window == 0 && s.kv >= s.n)          // all but the last item are full: item x ends before position kv - n + (x + 1) per
+        return last + floor_sum(items - 1, TILE, a.tok_per_item, s.kv - s.n + a.tok_per_item + TILE - 1);
+    int64_t sum = last;
+    for (int x = 0; x < items - 1; ++x) sum += item_tiles<TILE>(a, make_item(a, i, s, x));
+    return sum;
+}
+
+template <int TILE>
+__device__ __forceinline__ int64_t head_tiles(const AttnArgs& a)
+{
+    if (a.list_mode == LIST_PER_TOKEN) return static_cast<int64_t>(a.b.T) * (((a.s << a.page_shift) + TILE - 1) / TILE);
+    const int lane = threadIdx.x & 31;
+    int64_t sum = 0;
+    for (int i = lane; i < a.b.n_seqs; i += 32) sum += seq_tiles<TILE>(a, i);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    return sum;
+}
+
+// The item that holds tile number r of a key head, the number of its first tile and its tiles; a whole warp. False: no such tile.
+template <int TILE>
+__device__ __forceinline__ bool locate_tile(const AttnArgs& a, int64_t r, AttnItem& it, int64_t& first, int& n)
+{
+    const int lane = threadIdx.x & 31;
+    if (a.list_mode == LIST_PER_TOKEN) {
+        n = ((a.s << a.page_shift) + TILE - 1) / TILE;
+        const int64_t item = r / n;
+        first = item * n;
+        if (item >= a.b.T) return false;
+        const int seq = seq_of_row(a.b, static_cast<int>(item));
+        const SeqSpan s = load_seq(a.b, seq, a.status);
+        it = make_item(a, seq, s, static_cast<int>(item) - s.q0);
+        if (item < s.q0 || item >= s.q0 + s.n) it.n_tok = 0;
+        return true;
+    }
+    int64_t base = 0;
+    int seq = -1;
+    for (int i0 = 0; i0 < a.b.n_seqs && seq < 0; i0 += 32) {
+        const int64_t c = i0 + lane < a.b.n_seqs ? seq_tiles<TILE>(a, i0 + lane) : 0;
+        int64_t sum = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t up = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += up;
+        }
+        const uint32_t past = __ballot_sync(0xffffffffu, base + sum > r);
+        if (past) {
+            const int l = __ffs(past) - 1;
+            seq = i0 + l;
+            base += __shfl_sync(0xffffffffu, sum - c, l);
+        } else {
+            base += __shfl_sync(0xffffffffu, sum, 31);
+        }
+    }
+    if (seq < 0) return false;
+    const SeqSpan s = load_seq(a.b, seq, a.status);
+    const int items = seq_items(a, s);
+    for (int x0 = 0; x0 < items; x0 += 32) {
+        const int c = x0 + lane < items ? item_tiles<TILE>(a, make_item(a, seq, s, x0 + lane)) : 0;
+        int sum = c;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int up = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += up;
+        }
+        const uint32_t past = __ballot_sync(0xffffffffu, base + sum > r);
+        if (past) {
+            const int l = __ffs(past) - 1;
+            n = __shfl_sync(0xffffffffu, c, l);
+            first = base + __shfl_sync(0xffffffffu, sum - c, l);
+            it = make_item(a, seq, s, x0 + l);
+            return true;
+        }
+        base += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    return false;
+}
+
+// A piece of work of one thread block: tiles [t_lo, t_hi) of a unit; slot < 0: the whole unit.
+struct Segment {
+    AttnItem it;
+    int head, t_lo, t_hi, v_base, slot;
+};
+
+// What a thread block leaves for the join: the unit that began in its share and went on behind it (n_tok 0: there is none) and
+// the block that holds its last piece.
+struct Cut {
+    int32_t tok0, n_tok, head, last;
+    int32_t unused[4];
+};
+
+// Walks a block's segments; every call by a whole warp.
+template <int TILE>
+struct Walk {
+    int64_t per_head, share, at, end;       // share > 0: tile numbers; share 0: unit numbers
+    Cut cut;
+
+    __device__ __forceinline__ void start(const AttnArgs& a)
+    {
+        share = 0;
+        cut = Cut{0, 0, 0, 0, {0, 0, 0, 0}};
+        if (a.share_min > 0) {
+            per_head = head_tiles<TILE>(a);
+            const int64_t total = per_head * a.n_kv_heads;
+            share = max((total + a.grid - 1) / a.grid, static_cast<int64_t>(a.share_min));
+            at = blockIdx.x * share;
+            end = min(at + share, total);
+        } else {
+            at = blockIdx.x;
+            end = static_cast<int64_t>(a.n_items) * a.n_kv_heads;
+        }
+    }
+    __device__ __forceinline__ bool next(const AttnArgs& a, Segment& g)
+    {
+        while (at < end) {
+            if (share == 0) {
+                g.head = static_cast<int>(at % a.n_kv_heads);
+                const bool some = attn_item(a, static_cast<int>(at / a.n_kv_heads), g.it);
+                at += a.grid;
+                if (!some) continue;
+                g.t_lo = 0;
+                g.t_hi = item_tiles<TILE>(a, g.it);
+                g.slot = -1;
+            } else {
+                int64_t first;
+                int n;
+                g.head = static_cast<int>(at / per_head);
+                const int64_t head_at = g.head * per_head;
+                if (!locate_tile<TILE>(a, at - head_at, g.it, first, n)) return false;
+                first += head_at;
+                g.t_lo = static_cast<int>(at - first);
+                g.t_hi = static_cast<int>(min(first + n, end) - first);
+                const bool whole = g.t_lo == 0 && g.t_hi == n;
+                g.slot = whole ? -1 : 2 * static_cast<int>(blockIdx.x) + (first + n > end ? 1 : 0);
+                if (first + n > end && first >= blockIdx.x * share)
+                    cut = Cut{g.it.tok0, g.it.n_tok, g.head, static_cast<int32_t>((first + n - 1) / share), {0, 0, 0, 0}};
+                at = first + g.t_hi;
+                if (g.it.n_tok <= 0) continue;
+            }
+            g.v_base = a.list_mode == LIST_NONE ? first_seen(a, g.it) & ~(TILE - 1) : 0;
+            return true;
+        }
+        return false;
+    }
+    // Once all segments have been taken; one thread.
+    __device__ __forceinline__ void leave_cut(const AttnArgs& a) const
+    {
+        if (share > 0) reinterpret_cast<Cut*>(a.cuts)[blockIdx.x] = cut;
+    }
+};
 
 // ---- PTX wrappers -------------------------------------------------------------------------------
 namespace kv {

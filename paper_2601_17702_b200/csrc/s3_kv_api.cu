@@ -49,20 +49,19 @@ s3_status make_map(unsigned char (&map)[128], s3_dtype dtype, const void* base, 
 
 constexpr int kSplitRows = 16;             // rows per item up to which the split kernel serves
 constexpr int kTileRows = 128;
-constexpr int kMaxSplits = 256;
 
-// How an attention call is cut: which kernel, tokens per item, items, and the most splits it may use. None of it depends on the
-// device-side lengths, so the same numbers size the workspace.
+// How an attention call is cut. None of it depends on the device-side lengths.
 struct AttnPlan {
-    bool tile;
-    int tok_per_item, n_items, one_item_per_seq, max_splits;
+    bool tile;                             // tile kernel, else split kernel
+    int tok_per_item, n_items, one_item_per_seq;
+    int grid, share_min, rows_cap;
 };
 
-AttnPlan plan_attention(const s3_kv_batch& b, int group, int n_kv_heads, bool list_per_token)
+// keys: the most virtual keys an item can have.
+AttnPlan plan_attention(const s3_kv_batch& b, int group, int n_kv_heads, int list_mode, int64_t keys)
 {
     AttnPlan p;
-    const int n_sm = device_sm_count();
-    if (list_per_token) {
+    if (list_mode == LIST_PER_TOKEN) {
         p.tile = group > kSplitRows;
         p.tok_per_item = 1;
         p.n_items = b.T;
@@ -74,19 +73,30 @@ AttnPlan plan_attention(const s3_kv_batch& b, int group, int n_kv_heads, bool li
         p.one_item_per_seq = b.max_q <= p.tok_per_item;
         p.n_items = p.one_item_per_seq ? b.n_seqs : b.T / p.tok_per_item + b.n_seqs;
     }
-    // Splits fill the SMs when there are few items: up to eight thread blocks per SM in the split kernel (two run at a time; the
-    // rest evens out sequences of unequal length), two in the tile kernel (one runs at a time).
-    const int64_t blocks = static_cast<int64_t>(p.n_items) * n_kv_heads;
-    const int64_t want = (static_cast<int64_t>(p.tile ? 2 : 8) * n_sm + blocks - 1) / (blocks > 0 ? blocks : 1);
-    p.max_splits = static_cast<int>(want < 1 ? 1 : want > kMaxSplits ? kMaxSplits : want);
+    p.rows_cap = !p.tile ? kSplitRows : p.tok_per_item * group;
+    const int64_t places = (p.tile ? 1 : 2) * static_cast<int64_t>(device_sm_count());     // thread blocks that run at a time
+    const int64_t units = static_cast<int64_t>(p.n_items) * n_kv_heads, tiles = (keys + (p.tile ? 127 : 63)) / (p.tile ? 128 : 64);
+    // Shares end together whatever the lengths are, but cost a second launch and the partial results: about 6 tiles' time in the tile
+    // kernel, 12 in the split kernel. Units that are alike (lists; one sequence) stay whole where their rounds cost no more than
+    // that; units of several sequences, whose lengths the host does not see, when even the longest is short.
+    const int64_t extra = p.tile ? 6 : 12, rounds = (units + places - 1) / places;
+    const bool alike = list_mode != LIST_NONE || b.n_seqs == 1;
+    if (alike ? rounds * tiles <= units * tiles / places + extra : units <= places && tiles <= extra) {
+        p.grid = static_cast<int>(units < places ? units : places);
+        p.share_min = 0;
+    } else {
+        p.grid = static_cast<int>(places);
+        p.share_min = p.tile ? 2 : 4;
+    }
     return p;
 }
 
-size_t partial_bytes(const s3_kv_batch& b, int n_heads, int head_dim, int n_splits)
+// Partial results: two slots per thread block.
+size_t partial_bytes(const AttnPlan& p, int head_dim)
 {
-    if (n_splits <= 1) return 0;
-    const size_t rows = static_cast<size_t>(b.T) * n_heads * n_splits;
-    return round_up(rows * head_dim * 4, 256) + round_up(rows * 4, 256);
+    if (p.share_min == 0) return 0;
+    const size_t rows = 2 * static_cast<size_t>(p.grid) * p.rows_cap;
+    return round_up(rows * head_dim * 4, 256) + round_up(rows * 4, 256) + static_cast<size_t>(p.grid) * sizeof(Cut);
 }
 
 }  // namespace
@@ -168,7 +178,7 @@ s3_status attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const vo
     S3_TRY(check_rows("d_out", d_out, ld_out, n_heads, c.d.head_dim));
     S3_REQUIRE(d_ws != nullptr && ws_bytes >= S3_WS_HEADER_BYTES, S3_ERR_CAPACITY, "workspace missing or smaller than %d bytes", S3_WS_HEADER_BYTES);
     const int group = n_heads / c.d.n_kv_heads;
-    const AttnPlan p = plan_attention(b, group, c.d.n_kv_heads, list_mode == LIST_PER_TOKEN);
+    const AttnPlan p = plan_attention(b, group, c.d.n_kv_heads, list_mode, list_mode == LIST_NONE ? b.max_kv : static_cast<int64_t>(s) << c.page_shift);
 
     AttnArgs a;
     memset(&a, 0, sizeof(a));
@@ -181,7 +191,6 @@ s3_status attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const vo
     a.box_rows = c.box_rows;
     a.n_pages = c.d.n_pages;
     a.head_dim = c.d.head_dim;
-    a.scale = params->scale;
     a.scale_log2 = params->scale * kLog2e;
     a.causal = params->causal != 0;
     a.window = params->window;
@@ -199,29 +208,20 @@ s3_status attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const vo
     a.one_item_per_seq = p.one_item_per_seq;
     a.status = static_cast<uint32_t*>(d_ws);
 
-    // Virtual keys of the longest item, cut into splits of whole tiles that are not worth cutting further.
-    const int tile = p.tile ? 128 : 64, least = p.tile ? 512 : 256;
-    int64_t keys = list_mode == LIST_NONE ? b.max_kv : static_cast<int64_t>(s) << c.page_shift;
-    if (list_mode == LIST_NONE && params->window > 0) {
-        const int64_t seen = static_cast<int64_t>(params->window) + p.tok_per_item + tile;
-        if (seen < keys) keys = seen;
-    }
-    int64_t len = (keys + p.max_splits - 1) / p.max_splits;
-    if (len < least) len = least;
-    len = (len + tile - 1) / tile * tile;
-    a.split_len = static_cast<int32_t>(len);
-    a.n_splits = static_cast<int32_t>((keys + len - 1) / len);
-    if (a.n_splits < 1) a.n_splits = 1;
-    const size_t need = 256 + partial_bytes(b, n_heads, c.d.head_dim, a.n_splits);
-    S3_REQUIRE(a.n_splits == 1 || ws_bytes >= need, S3_ERR_CAPACITY, "workspace holds %zu bytes, %zu needed", ws_bytes, need);
-    if (a.n_splits > 1) {
-        const size_t rows = static_cast<size_t>(b.T) * n_heads * a.n_splits;
+    a.grid = p.grid;
+    a.share_min = p.share_min;
+    a.rows_cap = p.rows_cap;
+    const size_t need = 256 + partial_bytes(p, c.d.head_dim);
+    S3_REQUIRE(p.share_min == 0 || ws_bytes >= need, S3_ERR_CAPACITY, "workspace holds %zu bytes, %zu needed", ws_bytes, need);
+    if (p.share_min > 0) {
+        const size_t rows = 2 * static_cast<size_t>(p.grid) * p.rows_cap;
         a.part_o = reinterpret_cast<float*>(static_cast<unsigned char*>(d_ws) + 256);
         a.part_lse = reinterpret_cast<float*>(static_cast<unsigned char*>(d_ws) + 256 + round_up(rows * c.d.head_dim * 4, 256));
+        a.cuts = reinterpret_cast<int32_t*>(reinterpret_cast<unsigned char*>(a.part_lse) + round_up(rows * 4, 256));
     }
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
     S3_TRY(p.tile ? launch_attn_tile(c, a, st) : launch_attn_split(c, a, st));
-    return a.n_splits > 1 ? launch_attn_join(c, a, st) : S3_OK;
+    return p.share_min > 0 && p.grid > 1 ? launch_attn_join(c, a, p.tile, st) : S3_OK;
 }
 
 }  // namespace
@@ -281,9 +281,9 @@ size_t s3_kv_workspace_bytes(const s3_kv_cache* cache, const s3_kv_batch* batch,
     if (check_batch(cache, batch) != S3_OK || check_heads(cache, n_heads) != S3_OK) return 0;
     size_t most = 0;
     if (batch->T > 0 && batch->n_seqs > 0)
-        for (int per_token = 0; per_token < 2; ++per_token) {
-            const AttnPlan p = plan_attention(*batch, n_heads / cache->st.d.n_kv_heads, cache->st.d.n_kv_heads, per_token != 0);
-            const size_t bytes = partial_bytes(*batch, n_heads, cache->st.d.head_dim, p.max_splits);
+        for (int mode = LIST_NONE; mode <= LIST_PER_SEQ; ++mode) {
+            const AttnPlan p = plan_attention(*batch, n_heads / cache->st.d.n_kv_heads, cache->st.d.n_kv_heads, mode, INT32_MAX);
+            const size_t bytes = partial_bytes(p, cache->st.d.head_dim);
             if (bytes > most) most = bytes;
         }
     return 256 + most;
