@@ -1,12 +1,14 @@
 // Block selection: per new token and key head, the s blocks with the highest 8-bit score, the first and last ones included.
 //
-// A thread block takes TT tokens of one sequence and one key head. (1) The group's queries are summed in fixed point and coded
-// to 8 bits, one warp per token. (2) Threads walk the sequence's blocks: a block's 8-bit summary is read once into registers
-// and multiplied (dp4a, exact) with the codes of all TT tokens; the scores go to shared memory as order-preserving words
-// (forced blocks highest, invisible ones 0). (3) A warp per token selects: the s-th largest of the 32 lanes' maxima bounds the
-// s-th largest score from below, so one pass collects the few candidates above it in block order, and a bisection over their
-// bits finds the exact cut; ties at the cut go to the lowest blocks. More than 32 blocks, or more candidates than the buffer
-// holds, bisect over all scores instead.
+// A thread block takes up to TT tokens of one sequence and one key head. (1) The group's queries are summed in fixed point and
+// coded to 8 bits, one warp per token. (2) The codes of 16 tokens are one operand of an 8-bit mma.sync (exact 32-bit sums) whose
+// other operand, the codes of 8 blocks, goes from memory straight to registers: the two uint4 that a lane reads of its block's
+// code and of its tokens' codes hold the same dimensions, and in which order a dot product takes them does not matter. (An 8-bit
+// mma does 512 products per clock and scheduler, dp4a 64: 91 us per 2048 tokens x 8 heads x 512 blocks with dp4a.) The
+// scores go to shared memory as order-preserving words (forced blocks highest, invisible ones 0). (3) A warp per token
+// selects: each lane keeps two maxima, and the s-th largest of the 64 bounds the s-th largest score from below, so one pass
+// collects the few candidates above it in block order, and each then counts how many are better. 33 to 64 candidates, or (large
+// s, many equal scores) all scores, are bisected over their bits instead; ties always go to the lowest blocks.
 #include "s3_kernels.cuh"
 #include "s3_kv.cuh"
 
@@ -15,8 +17,9 @@ namespace {
 
 using kv::Half2Of;
 
-constexpr int CAND = 256;                   // candidates per warp
 constexpr int SCORE_BYTES = 96 << 10;       // shared memory for scores: two thread blocks per SM
+constexpr int MMA_TOKENS = 16;
+constexpr int CAND = 64;                    // candidates per warp
 
 struct SelectArgs {
     KvBatchDev b;
@@ -30,10 +33,13 @@ struct SelectArgs {
     uint32_t* status;
 };
 
-__device__ __forceinline__ uint32_t order_of(float x)
+// Order-preserving word of fl32(dot) * scale. |dot| < 2^22: adding it to the bits of 1.5 * 2^23 converts it exactly, without the
+// conversion unit; the multiply-add with +0 turns a -0 (scale 0) into the +0 that it equals.
+__device__ __forceinline__ uint32_t order_of(int dot, float scale)
 {
-    const uint32_t b = __float_as_uint(x + 0.0f);        // -0 counts as 0
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
+    const float x = __fmaf_rn(__fsub_rn(__int_as_float(0x4B400000 + dot), 12582912.0f), scale, 0.0f);
+    const int b = __float_as_int(x);
+    return static_cast<uint32_t>(b ^ ((b >> 31) | static_cast<int>(0x80000000u)));
 }
 
 // Largest v such that at least s of the n keys are >= v (n >= s).
@@ -77,32 +83,72 @@ __device__ __forceinline__ void select_row(const uint32_t* keys, int nb, int s, 
         for (int i = lane; i < s; i += 32) out[i] = i < nb ? i : -1;
         return;
     }
-    if (s <= 32) {
-        uint32_t best = 0;
-        for (int i = lane; i < nb; i += 32) best = max(best, keys[i]);
-        // the lanes' maxima in descending order over the lanes
-#pragma unroll
-        for (int size = 2; size <= 32; size <<= 1)
-#pragma unroll
-            for (int o = size >> 1; o > 0; o >>= 1) {
-                const uint32_t other = __shfl_xor_sync(0xffffffffu, best, o);
-                const bool keep_max = ((lane & o) == 0) == ((lane & size) == 0);
-                best = keep_max ? max(best, other) : min(best, other);
+    {
+        // four neighbouring blocks per lane and step; what a row holds past its blocks is ignored
+        const uint4* keys4 = reinterpret_cast<const uint4*>(keys);
+        auto four = [&](int i0) {
+            uint4 k = keys4[(i0 >> 2) + lane];
+            if (i0 + 128 > nb) {
+                const int left = nb - i0 - 4 * lane;
+                if (left < 1) k.x = 0;
+                if (left < 2) k.y = 0;
+                if (left < 3) k.z = 0;
+                if (left < 4) k.w = 0;
             }
-        const uint32_t bound = __shfl_sync(0xffffffffu, best, s - 1);
+            return k;
+        };
+        uint32_t best_a = 0, best_b = 0;                               // of this lane's even and odd pairs of blocks
+        for (int i0 = 0; i0 < nb; i0 += 128) {
+            const uint4 k = four(i0);
+            best_a = max(best_a, max(k.x, k.y));
+            best_b = max(best_b, max(k.z, k.w));
+        }
+        // the s-th largest of the 64 maxima, rounded down to its upper 17 bits
+        uint32_t bound = 0;
+#pragma unroll
+        for (int bit = 31; bit >= 15; --bit) {
+            const uint32_t t = bound | (1u << bit);
+            if (__popc(__ballot_sync(0xffffffffu, best_a >= t)) + __popc(__ballot_sync(0xffffffffu, best_b >= t)) >= s) bound = t;
+        }
+        bound = max(bound, 1u);
+        // candidate number c of the row, in block order, ends up in lane c
+        const uint32_t lower = (1u << lane) - 1;
         int n = 0;
-        for (int i0 = 0; i0 < nb && n <= CAND; i0 += 32) {
-            const bool in = i0 + lane < nb && keys[i0 + lane] >= bound;
-            const uint32_t m = __ballot_sync(0xffffffffu, in);
-            const int at = n + __popc(m & ((1u << lane) - 1));
-            if (in && at < CAND) cand[at] = static_cast<uint16_t>(i0 + lane);
-            n += __popc(m);
+        for (int i0 = 0; i0 < nb; i0 += 128) {
+            const uint4 k = four(i0);
+            const bool in[4] = {k.x >= bound, k.y >= bound, k.z >= bound, k.w >= bound};
+            int at = n;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const uint32_t all = __ballot_sync(0xffffffffu, in[x]);
+                at += __popc(all & lower);
+                n += __popc(all);
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                if (in[x] && at < CAND) cand[at] = static_cast<uint16_t>(i0 + 4 * lane + x);
+                at += in[x];
+            }
         }
         __syncwarp();
-        if (n <= CAND && bound > 0) {
+        const int num = lane < min(n, 32) ? cand[lane] : -1;
+        const uint32_t key = num >= 0 ? keys[num] : 0u;
+        __syncwarp();
+        if (n >= s && n <= 32) {
+            int better = 0;
+#pragma unroll
+            for (int c = 0; c < 32; ++c) {
+                const uint32_t k = __shfl_sync(0xffffffffu, key, c);       // 0 past the last candidate
+                better += k > key || (k == key && c < lane);
+            }
+            const bool take = lane < n && better < s;
+            const uint32_t taken = __ballot_sync(0xffffffffu, take);
+            if (take) out[__popc(taken & ((1u << lane) - 1))] = num;
+            return;
+        }
+        if (n > 32 && n <= CAND) {
             auto get = [&](int i) { return keys[cand[i]]; };
-            const uint32_t cut = n == s ? bound : cut_of(n, s, get);
-            emit(n, s, cut, get, [&](int i) { return static_cast<int32_t>(cand[i]); }, out);
+            emit(n, s, cut_of(n, s, get), get, [&](int i) { return static_cast<int32_t>(cand[i]); }, out);
             __syncwarp();
             return;
         }
@@ -112,13 +158,13 @@ __device__ __forceinline__ void select_row(const uint32_t* keys, int nb, int s, 
 }
 
 template <class T, int D, int TT, int THREADS>
-__global__ void __launch_bounds__(THREADS) select_kernel(const SelectArgs a)
+__global__ void __launch_bounds__(THREADS, TT == 16 ? 5 : 2) select_kernel(const SelectArgs a)
 {
-    constexpr int W = D / 4;                                  // 32-bit words of a code
+    constexpr int W = D / 4, WARPS = THREADS / 32;            // 32-bit words of a code
     extern __shared__ __align__(16) unsigned char smem[];
-    uint32_t* codes = reinterpret_cast<uint32_t*>(smem);      // [TT][W]
-    uint16_t* cand = reinterpret_cast<uint16_t*>(smem + TT * D);      // [warps][CAND]
-    uint32_t* keys = reinterpret_cast<uint32_t*>(smem + TT * D + (THREADS / 32) * CAND * 2);   // [TT][nb_cap]
+    uint32_t* codes = reinterpret_cast<uint32_t*>(smem);      // [16][W], rows past the tokens zero
+    uint32_t* keys = reinterpret_cast<uint32_t*>(smem + MMA_TOKENS * D);   // [TT][nb_cap]
+    __shared__ uint16_t cand[WARPS][CAND];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int head = blockIdx.x % a.n_kv_heads, item = blockIdx.x / a.n_kv_heads;
     int seq = item, idx = 0;
@@ -131,7 +177,11 @@ __global__ void __launch_bounds__(THREADS) select_kernel(const SelectArgs a)
     if (n_tok <= 0) return;
     const int tok0 = s.q0 + idx * TT, pos0 = s.kv - s.n + idx * TT;
 
-    for (int tt = warp; tt < n_tok; tt += THREADS / 32) {
+    for (int tt = warp; tt < MMA_TOKENS; tt += WARPS) {
+        if (tt >= n_tok) {
+            if (lane < W) codes[tt * W + lane] = 0u;
+            continue;
+        }
         using H = Half2Of<T>;
         int q[4] = {0, 0, 0, 0};
         if (lane < W) {
@@ -143,11 +193,11 @@ __global__ void __launch_bounds__(THREADS) select_kernel(const SelectArgs a)
             }
         }
         const int most = __reduce_max_sync(0xffffffffu, max(max(abs(q[0]), abs(q[1])), max(abs(q[2]), abs(q[3]))));
-        const float m = __int2float_rn(max(most, 1));
+        const float m = __int2float_rn(max(most, 1)), inv = 1.0f / m;
         uint32_t w = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int c = static_cast<int>(rintf(__fdiv_rn(__fmul_rn(__int2float_rn(q[i]), 127.0f), m)));
+            const int c = kv::code_of(q[i], m, inv);
             w |= (static_cast<uint32_t>(c) & 0xffu) << (8 * i);
         }
         if (lane < W) codes[tt * W + lane] = w;
@@ -156,45 +206,74 @@ __global__ void __launch_bounds__(THREADS) select_kernel(const SelectArgs a)
 
     const int last = pos0 + n_tok - 1;
     const int nb = last < 0 ? 0 : (last >> a.page_shift) + 1;        // blocks that some token of the tile sees
-    for (int j = threadIdx.x; j < nb; j += THREADS) {
-        const int page = a.b.pages[seq * a.b.ld_pages + j];
-        uint4 c[W / 4];
-        float scale = 0.0f;
-        if (page >= 0 && page < a.n_pages) {
-            const int64_t at = static_cast<int64_t>(page) * a.n_kv_heads + head;
-            const uint4* src = reinterpret_cast<const uint4*>(a.code + at * D);
+    const int row = lane >> 2, quad = lane & 3;
+    constexpr int Q = D / 64;                                         // uint4 per lane and row
+    uint4 ta[Q], tb[Q];                                               // tokens row and row + 8
 #pragma unroll
-            for (int i = 0; i < W / 4; ++i) c[i] = __ldg(src + i);
-            scale = __ldg(a.scale + at);
-        } else {
+    for (int x = 0; x < Q; ++x) {
+        ta[x] = *reinterpret_cast<const uint4*>(codes + row * W + (x * 4 + quad) * 4);
+        tb[x] = TT > 8 ? *reinterpret_cast<const uint4*>(codes + (row + 8) * W + (x * 4 + quad) * 4) : make_uint4(0, 0, 0, 0);
+    }
+    const int32_t* table = a.b.pages + seq * a.b.ld_pages;
+    const int8_t* my_code = a.code + head * D + quad * 16;            // of page 0
+    const float* my_scale = a.scale + head;
+    const int page_pitch = a.n_kv_heads * D;
+    auto fetch = [&](int g, uint4 (&c)[Q], float& scale) {            // block 8 g + row
+        const int j = g * 8 + row;
+        scale = 0.0f;
+#pragma unroll
+        for (int x = 0; x < Q; ++x) c[x] = make_uint4(0, 0, 0, 0);
+        if (j >= nb) return;
+        const int page = __ldg(table + j);
+        if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(a.n_pages)) {
             dev_set_error(a.status, DEV_BAD_PAGE);
-#pragma unroll
-            for (int i = 0; i < W / 4; ++i) c[i] = make_uint4(0, 0, 0, 0);
+            return;
         }
-#pragma unroll 4
-        for (int tt = 0; tt < TT; ++tt) {
-            if (tt >= n_tok) break;
-            const uint4* q4 = reinterpret_cast<const uint4*>(codes + tt * W);
-            int d0 = 0, d1 = 0;
+        const int8_t* src = my_code + static_cast<int64_t>(page) * page_pitch;
 #pragma unroll
-            for (int i = 0; i < W / 4; ++i) {
-                const uint4 q = q4[i];
-                d0 = __dp4a(static_cast<int>(c[i].x), static_cast<int>(q.x), d0);
-                d1 = __dp4a(static_cast<int>(c[i].y), static_cast<int>(q.y), d1);
-                d0 = __dp4a(static_cast<int>(c[i].z), static_cast<int>(q.z), d0);
-                d1 = __dp4a(static_cast<int>(c[i].w), static_cast<int>(q.w), d1);
+        for (int x = 0; x < Q; ++x) c[x] = __ldg(reinterpret_cast<const uint4*>(src + x * 64));
+        scale = __ldg(my_scale + static_cast<int64_t>(page) * a.n_kv_heads);
+    };
+    auto mma = [](int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+        asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    };
+    const int own_first = pos0 >> a.page_shift;                        // the tile's lowest own block
+    uint4 next[Q];
+    float next_scale;
+    fetch(warp, next, next_scale);
+    for (int g = warp; g * 8 < nb; g += WARPS) {
+        uint4 c[Q];
+#pragma unroll
+        for (int x = 0; x < Q; ++x) c[x] = next[x];
+        const float scale = next_scale;
+        fetch(g + WARPS, next, next_scale);                            // the next group is on its way meanwhile
+        int dot[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int x = 0; x < Q; ++x) {
+            mma(dot, ta[x].x, tb[x].x, ta[x].y, tb[x].y, c[x].x, c[x].y);
+            mma(dot, ta[x].z, tb[x].z, ta[x].w, tb[x].w, c[x].z, c[x].w);
+        }
+        const float s0 = __shfl_sync(0xffffffffu, scale, quad * 8), s1 = __shfl_sync(0xffffffffu, scale, quad * 8 + 4);
+        uint32_t* to = keys + row * a.nb_cap + g * 8 + quad * 2;
+        uint32_t key[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) key[x] = order_of(dot[x], x & 1 ? s1 : s0);
+        if (g * 8 < a.n_first || g * 8 + 7 > own_first - a.n_last || own_first < 0) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const int own = (pos0 + row + (x >> 1) * 8) >> a.page_shift, j = g * 8 + quad * 2 + (x & 1);
+                if (j < a.n_first || j > own - a.n_last) key[x] = 0xffffffffu;
+                if (j > own) key[x] = 0u;                              // own < 0 at a negative position: nothing is visible
             }
-            const int own = (pos0 + tt) >> a.page_shift;              // < 0 at a negative position: nothing is visible
-            uint32_t key = order_of(__fmul_rn(__int2float_rn(d0 + d1), scale));
-            if (j < a.n_first || j > own - a.n_last) key = 0xffffffffu;
-            if (j > own) key = 0u;
-            keys[tt * a.nb_cap + j] = key;
         }
+        if (row < TT) *reinterpret_cast<uint2*>(to) = make_uint2(key[0], key[1]);
+        if (TT > 8) *reinterpret_cast<uint2*>(to + 8 * a.nb_cap) = make_uint2(key[2], key[3]);
     }
     __syncthreads();
-    for (int tt = warp; tt < n_tok; tt += THREADS / 32) {
+    for (int tt = warp; tt < n_tok; tt += WARPS) {
         const int pos = pos0 + tt;
-        select_row(keys + tt * a.nb_cap, pos < 0 ? 0 : (pos >> a.page_shift) + 1, a.s, cand + warp * CAND,
+        select_row(keys + tt * a.nb_cap, pos < 0 ? 0 : (pos >> a.page_shift) + 1, a.s, cand[warp],
                    a.blocks + (static_cast<int64_t>(tok0 + tt) * a.n_kv_heads + head) * a.s);
     }
 }
@@ -202,7 +281,7 @@ __global__ void __launch_bounds__(THREADS) select_kernel(const SelectArgs a)
 template <class T, int D, int TT, int THREADS>
 s3_status launch_one(SelectArgs& a, cudaStream_t stream)
 {
-    const size_t smem = static_cast<size_t>(TT) * D + (THREADS / 32) * CAND * 2 + static_cast<size_t>(TT) * a.nb_cap * 4;
+    const size_t smem = static_cast<size_t>(MMA_TOKENS) * D + static_cast<size_t>(TT) * a.nb_cap * 4;
     static bool raised[64] = {};                 // the attribute is kept per device; setting it twice does no harm
     int dev = 0;
     S3_CUDA_TRY(cudaGetDevice(&dev));
@@ -246,7 +325,8 @@ s3_status launch_block_select(const KvCacheState& c, const KvBatchDev& b, const 
     a.s = s;
     a.n_first = n_first;
     a.n_last = n_last;
-    a.nb_cap = ((b.max_kv + c.d.page_size - 1) >> c.page_shift) | 1;     // odd row pitch: rows start in different banks
+    // words per row: whole steps of 128 blocks, and 8 more than a multiple of 32, so that 4 rows of a store fall into different banks
+    a.nb_cap = (((b.max_kv + c.d.page_size - 1) >> c.page_shift) + 127) / 128 * 128 + 8;
     a.blocks = d_blocks;
     a.status = d_status;
     const bool wide = c.d.head_dim == 128;

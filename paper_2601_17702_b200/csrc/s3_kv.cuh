@@ -440,10 +440,20 @@ struct Half2Of<__half> {
     static __device__ __forceinline__ float hi(uint32_t v) { return __half2float(__ushort_as_half(static_cast<unsigned short>(v >> 16))); }
 };
 
+// rint(4096 clamp(x, -2047, 2047)), NaN -> 0: the conversion saturates and takes NaN to 0, the limit is a whole number of steps.
 __device__ __forceinline__ int fixed_of(float x)
 {
-    if (x != x) return 0;
-    return __float2int_rn(__fmul_rn(fminf(fmaxf(x, -kSumLimit), kSumLimit), kSumSteps));
+    constexpr int limit = static_cast<int>(kSumLimit * kSumSteps);
+    return min(max(__float2int_rn(__fmul_rn(x, kSumSteps)), -limit), limit);
+}
+
+// rint(127 total / most) as two fp32 roundings (the product's and the quotient's) define it. The reciprocal is off by a few units
+// in the last place, which shows only next to a half: there the quotient is taken.
+__device__ __forceinline__ int code_of(int total, float most, float inv)
+{
+    const float x = __fmul_rn(__int2float_rn(total), 127.0f), r = x * inv, n = rintf(r);
+    if (fabsf(fabsf(r - n) - 0.5f) > 1e-3f) return static_cast<int>(n);
+    return static_cast<int>(rintf(__fdiv_rn(x, most)));
 }
 
 }  // namespace kv
