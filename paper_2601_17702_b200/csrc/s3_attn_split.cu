@@ -109,6 +109,10 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
 
+    // token and head of a query row, row < 16: an integer division costs some 100 clocks
+    const uint32_t group_inv = (65536u + a.group - 1) / a.group;
+    auto token_of = [&](int row) { return static_cast<int>(row * group_inv >> 16); };
+    auto head_of = [&](int row) { return row - token_of(row) * a.group; };
     auto give_up = [&](uint32_t code) {
         if (lane == 0) { dev_set_error(a.status, code); *abort_flag = 1; }
     };
@@ -118,39 +122,40 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
         const int box = a.box_rows, per_tile = TILE / box, group_tiles = 32 / per_tile;
         const int lane_tile = lane / per_tile, lane_box = lane % per_tile;
         int tiles = 0, units = 0;                                     // pushed so far
-        bool ok = true, met = false;
+        bool ok = true;
+        prefetch_tables(a);
+        if (lane == 0) {
+            prefetch_map(maps.k);
+            prefetch_map(maps.v);
+        }
         Walk<TILE> walk;
         Segment g;
         walk.start(a);
-        while (ok && walk.next(a, g)) {
+        // A lane per box: the lanes read the table entries of the next 32 boxes together, one group ahead of the copies, so that
+        // no copy waits for its page number. The next segment is looked up while the ring is full.
+        auto look_up = [&](const Segment& of, int t, int& page, int& pos) {       // this lane's box of tile t + lane_tile
+            const int v = of.v_base + (of.t_lo + t + lane_tile) * TILE + lane_box * box;
+            page = pos = -1;
+            if (t + lane_tile >= of.t_hi - of.t_lo) return;
+            if (a.list_mode == LIST_NONE) pos = v <= of.it.pos_last ? v : -1;
+            else if (v < a.s << a.page_shift) {
+                const int id = a.lists[(static_cast<int64_t>(of.it.list) * a.list_heads + (a.list_heads == 1 ? 0 : of.head)) * a.s + (v >> a.page_shift)];
+                // a block all of whose positions are out of sight counts as not listed
+                if (id >= 0 && of.it.pos_last >= 0 && id <= (of.it.pos_last >> a.page_shift) && ((id + 1) << a.page_shift) > first_seen(a, of.it))
+                    pos = (id << a.page_shift) + (v & (a.page_size - 1));
+            }
+            if (pos < 0 || pos >= of.it.kv) { pos = -1; return; }
+            const int p = a.b.pages[of.it.seq * a.b.ld_pages + (pos >> a.page_shift)];
+            page = p < 0 || p >= a.n_pages ? a.n_pages : p;            // beyond the map: reads as zeros
+        };
+        Segment ahead;
+        int page, pos, next_page = -1, next_pos = -1;
+        bool some = walk.next(a, g);
+        if (some) look_up(g, 0, next_page, next_pos);
+        __syncthreads();                                              // the barriers exist; the first reads ran meanwhile
+        while (ok && some) {
             const AttnItem& it = g.it;
-            const int head = g.head, pos_last = it.pos_last, seen_lo = first_seen(a, it), n_tiles = g.t_hi - g.t_lo, rows = it.n_tok * a.group;
-            const int v_lo = g.v_base + g.t_lo * TILE, v_hi = min(v_lo + n_tiles * TILE, a.list_mode == LIST_NONE ? pos_last + 1 : a.s << a.page_shift);
-            const int32_t* table = a.b.pages + it.seq * a.b.ld_pages;
-            const int32_t* list = a.lists + (static_cast<int64_t>(it.list) * a.list_heads + (a.list_heads == 1 ? 0 : head)) * a.s;
-
-            // A lane per box: the lanes read the table entries of the next 32 boxes together, one group ahead of the copies,
-            // so that no copy waits for its page number.
-            auto entry = [&](int t, int& page, int& pos) {             // this lane's box of tile t + lane_tile
-                const int v = v_lo + (t + lane_tile) * TILE + lane_box * box;
-                page = pos = -1;
-                if (v >= v_hi) return;
-                if (a.list_mode == LIST_NONE) pos = v;
-                else {
-                    const int id = list[v >> a.page_shift];
-                    // a block all of whose positions are out of sight counts as not listed
-                    if (id >= 0 && pos_last >= 0 && id <= (pos_last >> a.page_shift) && ((id + 1) << a.page_shift) > seen_lo)
-                        pos = (id << a.page_shift) + (v & (a.page_size - 1));
-                }
-                if (pos < 0 || pos >= it.kv) { pos = -1; return; }
-                const int p = table[pos >> a.page_shift];
-                page = p < 0 || p >= a.n_pages ? a.n_pages : p;        // beyond the map: reads as zeros
-            };
-            int page, pos, next_page, next_pos;
-            entry(0, next_page, next_pos);
-            if (!met) __syncthreads();                                // the barriers exist; the first reads ran meanwhile
-            met = true;
-
+            const int head = g.head, pos_last = it.pos_last, n_tiles = g.t_hi - g.t_lo, rows = it.n_tok * a.group;
             const int ub = units & 1;
             if (units >= 2 && !__all_sync(0xffffffffu, mbar_wait(&unit_empty[ub], ((units >> 1) - 1) & 1, abort_flag))) {
                 give_up(DEV_TIMEOUT_SMEM_EMPTY);
@@ -162,8 +167,7 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
             }
             __syncwarp();
             if (lane < rows) {
-                const T* src = static_cast<const T*>(a.q) + static_cast<int64_t>(it.tok0 + lane / a.group) * a.ldq +
-                               static_cast<int64_t>(head * a.group + lane % a.group) * D;
+                const T* src = static_cast<const T*>(a.q) + static_cast<int64_t>(it.tok0 + token_of(lane)) * a.ldq + (head * a.group + head_of(lane)) * D;
                 bulk_load(ring + L::Q + (ub * NT * 8 + lane) * L::Q_PITCH, src, D * 2, &unit_full[ub]);
             }
             ++units;
@@ -172,7 +176,8 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                 page = next_page;
                 pos = next_pos;
                 if (page == a.n_pages) dev_set_error(a.status, DEV_BAD_PAGE);
-                entry(t0 + group_tiles, next_page, next_pos);
+                const bool last_group = t0 + group_tiles >= n_tiles;
+                if (!last_group) look_up(g, t0 + group_tiles, next_page, next_pos);
                 for (int t = t0; t < min(n_tiles, t0 + group_tiles); ++t) {
                     const int st = tiles % STAGES, round = tiles / STAGES;
                     if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(&empty_bar[st], (round - 1) & 1, abort_flag))) {
@@ -181,11 +186,14 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                         break;
                     }
                     const bool here = lane_tile == t - t0, mine = here && page >= 0;
-                    if (here)
-                        for (int x = 0; x < box / 16; ++x) {
+                    if (here) {
+                        const int units16 = box / 16;
+#pragma unroll
+                        for (int x = 0; x < TILE / 16; ++x) {
                             const int at = pos + 16 * x;               // whole 16-key units that no row can see are skipped
-                            pos16[st][lane_box * (box / 16) + x] = mine && at <= pos_last && at < it.kv ? at : -1;
+                            if (x < units16) pos16[st][lane_box * units16 + x] = mine && at <= pos_last && at < it.kv ? at : -1;
                         }
+                    }
                     const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, mine));
                     __syncwarp();
                     if (lane == 0) {
@@ -195,18 +203,20 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                     ++tiles;
                     __syncwarp();
                     if (mine) {
-                        unsigned char* dst = ring + st * L::STAGE + lane_box * box * 128;
+                        // a box holds its rows' first halves, then their second ones
+                        unsigned char* dst = ring + st * L::STAGE + lane_box * box * D * 2;
                         const int row = pos & (a.page_size - 1);
-#pragma unroll
-                        for (int h = 0; h < D / 64; ++h) {
-                            tma_load_4d(dst + h * TILE * 128, maps.k, h * 64, row, head, page, &full_bar[st]);
-                            tma_load_4d(dst + TILE * D * 2 + h * TILE * 128, maps.v, h * 64, row, head, page, &full_bar[st]);
-                        }
+                        tma_load_rows(dst, maps.k, row, head, page, &full_bar[st]);
+                        tma_load_rows(dst + TILE * D * 2, maps.v, row, head, page, &full_bar[st]);
+                    }
+                    if (last_group && t == min(t0 + STAGES - 1, n_tiles - 1)) {
+                        some = walk.next(a, ahead);
+                        if (some) look_up(ahead, 0, next_page, next_pos);
                     }
                 }
             }
+            g = ahead;
         }
-        if (!met) __syncthreads();
         if (lane == 0) walk.leave_cut(a);
         const int ub = units & 1;
         if (ok && units >= 2 && !__all_sync(0xffffffffu, mbar_wait(&unit_empty[ub], ((units >> 1) - 1) & 1, abort_flag)))
@@ -226,6 +236,9 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
         const int mi = lane >> 3, mr = lane & 7;
         const int k_row = warp * 16 + (mi & 1) * 8 + mr, k_chunk = mi >> 1;       // K as A: (keys 0-7 | 8-15) x (d 0-7), then d 8-15
         const int v_row = warp * 16 + (mi >> 1) * 8 + mr, v_chunk = mi & 1;       // V^T as A: (d 0-7 | 8-15) x (keys 0-7), then 8-15
+        // where this lane's rows are in a tile of boxes, and how far apart a row's halves
+        const int box = a.box_rows, half_pitch = box * 128;
+        const uint32_t k_off = k_row / box * (box * D * 2) + k_row % box * 128, v_off = v_row / box * (box * D * 2) + v_row % box * 128;
         float* slot0 = reinterpret_cast<float*>(ring + L::SLOTS);
         float* slot1 = reinterpret_cast<float*>(ring + L::SLOTS + L::SLOT);
         int tiles = 0;
@@ -251,7 +264,7 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int row = n * 8 + quad * 2 + i;
-                    qpos[n][i] = row >= info.rows ? -1 : a.causal ? info.pos0 + row / a.group : info.pos0;
+                    qpos[n][i] = row >= info.rows ? -1 : a.causal ? info.pos0 + token_of(row) : info.pos0;
                 }
             }
             float o[NT][D / 16][4], m[NT][2], l[NT][2];
@@ -277,9 +290,9 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                         // values past the last position may hold anything: zero their rows
                         const int first = info.kv - pos;
                         for (int x = lane; x < (16 - first) * (D / 8); x += 32) {
-                            const int rr = first + x / (D / 8), c = x % (D / 8);
-                            *reinterpret_cast<uint4*>(tile + TILE * D * 2 + (c >> 3) * TILE * 128 + (warp * 16 + rr) * 128 + (c & 7) * 16) =
-                                make_uint4(0, 0, 0, 0);
+                            const int rr = warp * 16 + first + x / (D / 8), c = x % (D / 8);
+                            *reinterpret_cast<uint4*>(tile + TILE * D * 2 + rr / box * (box * D * 2) + (c >> 3) * half_pitch + rr % box * 128 +
+                                                      (c & 7) * 16) = make_uint4(0, 0, 0, 0);
                         }
                         fence_async_smem();
                         __syncwarp();
@@ -293,7 +306,7 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                     for (int k = 0; k < D / 16; ++k) {
                         uint32_t x[4];
                         const int c = k * 2 + k_chunk;
-                        ldsm4(x, ks + (c >> 3) * TILE * 128 + k_row * 128 + (((c & 7) ^ (k_row & 7)) << 4));
+                        ldsm4(x, ks + k_off + (c >> 3) * half_pitch + (((c & 7) ^ (k_row & 7)) << 4));
 #pragma unroll
                         for (int n = 0; n < NT; ++n) mma16816<T>(sc[n], x, q[n][k][0], q[n][k][1]);
                     }
@@ -344,7 +357,7 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                     for (int k = 0; k < D / 16; ++k) {
                         uint32_t x[4];
                         const int c = k * 2 + v_chunk;
-                        ldsm4_t(x, vs + (c >> 3) * TILE * 128 + v_row * 128 + (((c & 7) ^ (v_row & 7)) << 4));
+                        ldsm4_t(x, vs + v_off + (c >> 3) * half_pitch + (((c & 7) ^ (v_row & 7)) << 4));
 #pragma unroll
                         for (int n = 0; n < NT; ++n) mma16816<T>(o[n][k], x, p[n][0], p[n][1]);
                     }
@@ -432,10 +445,10 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                         inv[n][i] = l[n][i] == 0.0f ? 0.0f : 1.0f / l[n][i];
                         const int row = n * 8 + quad * 2 + i;
                         if (r8 == 0 && row < info.rows) {
-                            const int64_t out_row = static_cast<int64_t>(info.tok0 + row / a.group) * a.n_heads + info.head * a.group + row % a.group;
+                            const int64_t out_row = static_cast<int64_t>(info.tok0 + token_of(row)) * a.n_heads + info.head * a.group + head_of(row);
                             const float lse2 = l[n][i] == 0.0f ? -INFINITY : m[n][i] + log2f(l[n][i]);
                             if (info.slot >= 0) a.part_lse[info.slot * a.rows_cap + row] = lse2;
-                            else if (a.lse) a.lse[out_row] = lse2 / kLog2e;
+                            else if (a.lse) a.lse[out_row] = lse2 * kLn2;
                         }
                     }
 #pragma unroll
@@ -445,14 +458,16 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
 #pragma unroll
                         for (int j = 0; j < 4; ++j) at(slot0, n, k, j) = l[n][j & 1] == 0.0f ? 0.0f : o[n][k][j] * inv[n][j & 1];
                 __syncwarp();
-                for (int x = lane; x < info.rows * (D / 4); x += 32) {
-                    const int row = x / (D / 4), c = x % (D / 4) * 4;
+                // whole rows, 32 / (D / 4) at a time
+                constexpr int LANES = D / 4, STEP = 32 / LANES;
+                const int c = lane % LANES * 4;
+                for (int row = lane / LANES; row < info.rows; row += STEP) {
                     const float4 y = *reinterpret_cast<const float4*>(slot0 + row * L::PITCH + c);
-                    const int tok = info.tok0 + row / a.group, h = info.head * a.group + row % a.group;
                     if (info.slot >= 0) {
                         *reinterpret_cast<float4*>(a.part_o + (static_cast<int64_t>(info.slot) * a.rows_cap + row) * D + c) = y;
                     } else {
-                        T* dst = static_cast<T*>(a.out) + static_cast<int64_t>(tok) * a.ld_out + static_cast<int64_t>(h) * D + c;
+                        T* dst = static_cast<T*>(a.out) + static_cast<int64_t>(info.tok0 + token_of(row)) * a.ld_out +
+                                 (info.head * a.group + head_of(row)) * D + c;
                         *reinterpret_cast<uint2*>(dst) = make_uint2(Half2Of<T>::pack(y.x, y.y), Half2Of<T>::pack(y.z, y.w));
                     }
                 }
@@ -518,7 +533,7 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttnA
         T* dst = static_cast<T*>(a.out) + tok * a.ld_out + h * D + lane * N;
 #pragma unroll
         for (int j = 0; j < N; j += 2) *reinterpret_cast<uint32_t*>(dst + j) = Half2Of<T>::pack(y[j] * inv, y[j + 1] * inv);
-        if (lane == 0 && a.lse) a.lse[tok * a.n_heads + h] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) / kLog2e;
+        if (lane == 0 && a.lse) a.lse[tok * a.n_heads + h] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * kLn2;
     }
 }
 
@@ -534,8 +549,8 @@ s3_status launch_split(const KvCacheState& c, const AttnArgs& a, cudaStream_t st
         if (dev < 64) raised[dev] = true;
     }
     Maps maps;
-    memcpy(maps.k, c.map_k, sizeof(maps.k));
-    memcpy(maps.v, c.map_v, sizeof(maps.v));
+    memcpy(maps.k, c.wide_k, sizeof(maps.k));
+    memcpy(maps.v, c.wide_v, sizeof(maps.v));
     split_kernel<T, D, NT><<<a.grid, THREADS, L::TOTAL, stream>>>(maps, a);
     S3_CUDA_TRY(cudaGetLastError());
     return S3_OK;

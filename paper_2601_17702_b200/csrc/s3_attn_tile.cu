@@ -309,6 +309,12 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
             // ---------------- producer ----------------
             // A lane per box: the lanes read the table entries of the next 32 boxes together, a group of tiles ahead of the
             // copies (one lane reading an entry before each copy bound the kernel at 2.5 us per key tile).
+            prefetch_tables(a);
+            if (lane == 0) {
+                prefetch_map(maps.k);
+                prefetch_map(maps.v);
+                prefetch_map(maps.q);
+            }
             Walk<BN> walk;
             Segment g, g_next;
             walk.start(a);
@@ -684,7 +690,7 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
                 const float lse2 = empty ? -INFINITY : m + log2f(l);
                 if (live) {
                     if (info.slot >= 0) a.part_lse[part] = lse2;
-                    else if (a.lse) a.lse[out_row] = lse2 / kLog2e;
+                    else if (a.lse) a.lse[out_row] = lse2 * kLn2;
                 }
                 // a store's lane writes piece lane % 8 of the lines of rows x + 8 (lane / 8)
                 auto scaled = [&](int c, float (&o)[32]) {             // 32 results of this lane's row

@@ -10,14 +10,15 @@
 
 namespace s3 {
 
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSumSteps = 4096.0f, kSumLimit = 2047.0f;   // fixed point of the summaries and of the summed queries
 
 struct KvCacheState {
     s3_kv_cache_desc d;
     int page_shift;
     int box_rows;                                   // rows of one TMA box: min(page_size, 64)
-    alignas(64) unsigned char map_k[128], map_v[128];
+    alignas(64) unsigned char map_k[128], map_v[128];     // (column, row, head, page), box 64 columns
+    alignas(64) unsigned char wide_k[128], wide_v[128];   // (column of a half, row, half, head, page), box whole rows
 };
 
 struct KvBatchDev {
@@ -93,7 +94,9 @@ enum { LIST_NONE = 0, LIST_PER_TOKEN = 1, LIST_PER_SEQ = 2 };
 // are taken in tiles from the first one that some row of the item sees.
 //
 // The grid's thread blocks share the work in one of two ways, which the host chooses:
-//   share = 0   unit u = (item, key head), whole, goes to block u mod grid;
+//   share = 0   unit u = (key head, item), whole, goes to block u mod grid; key head by key head, so that the blocks are at work on
+//               the keys of one head or two, which the L2 cache holds when a token's list picks among many (1024 tokens x 16 of
+//               512 blocks: 360 -> 240 us);
 //   share > 0   the tiles of all units, laid end to end (key head by key head, item by item), are cut into equal shares of `share`
 //               tiles or less, one per block, whatever the lengths are. A unit that a cut divides is worked on in pieces; a
 //               piece's result goes to a slot of its block (each has at most two pieces: one that began before its share and
@@ -194,9 +197,8 @@ __device__ __forceinline__ int64_t floor_sum(uint32_t n, uint32_t m, uint32_t a,
 
 // Tiles of one key head over the items of sequence i.
 template <int TILE>
-__device__ __forceinline__ int64_t seq_tiles(const AttnArgs& a, int i)
+__device__ __forceinline__ int64_t seq_tiles(const AttnArgs& a, int i, const SeqSpan& s)
 {
-    const SeqSpan s = load_seq(a.b, i, nullptr);
     const int items = seq_items(a, s);
     if (items == 0) return 0;
     const int last = item_tiles<TILE>(a, make_item(a, i, s, items - 1));
@@ -209,26 +211,43 @@ __device__ __forceinline__ int64_t seq_tiles(const AttnArgs& a, int i)
     return sum;
 }
 
-template <int TILE>
-__device__ __forceinline__ int64_t head_tiles(const AttnArgs& a)
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b)        // of non-negative numbers, mostly small ones
 {
-    if (a.list_mode == LIST_PER_TOKEN) return static_cast<int64_t>(a.b.T) * (((a.s << a.page_shift) + TILE - 1) / TILE);
-    const int lane = threadIdx.x & 31;
-    int64_t sum = 0;
-    for (int i = lane; i < a.b.n_seqs; i += 32) sum += seq_tiles<TILE>(a, i);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    return sum;
+    return ((a | b) >> 32) == 0 ? static_cast<uint32_t>(a) / static_cast<uint32_t>(b) : a / b;
 }
 
-// The item that holds tile number r of a key head, the number of its first tile and its tiles; a whole warp. False: no such tile.
+// Sequences of a batch, 32 at a time, one per lane: lengths and the tiles up to and with each.
+struct SeqLanes {
+    SeqSpan span;
+    int64_t tiles, upto;
+};
+
 template <int TILE>
-__device__ __forceinline__ bool locate_tile(const AttnArgs& a, int64_t r, AttnItem& it, int64_t& first, int& n)
+__device__ __forceinline__ SeqLanes load_lanes(const AttnArgs& a, int i0)
+{
+    const int lane = threadIdx.x & 31;
+    SeqLanes q;
+    q.span = SeqSpan{0, 0, 0};
+    if (i0 + lane < a.b.n_seqs) q.span = load_seq(a.b, i0 + lane, a.status);
+    q.tiles = seq_tiles<TILE>(a, i0 + lane, q.span);
+    q.upto = q.tiles;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t up = __shfl_up_sync(0xffffffffu, q.upto, o);
+        if (lane >= o) q.upto += up;
+    }
+    return q;
+}
+
+// The item that holds tile number r of a key head, the number of its first tile and its tiles; a whole warp. `lanes` holds the
+// first 32 sequences. False: no such tile.
+template <int TILE>
+__device__ __forceinline__ bool locate_tile(const AttnArgs& a, const SeqLanes& lanes, int64_t r, AttnItem& it, int64_t& first, int& n)
 {
     const int lane = threadIdx.x & 31;
     if (a.list_mode == LIST_PER_TOKEN) {
         n = ((a.s << a.page_shift) + TILE - 1) / TILE;
-        const int64_t item = r / n;
+        const int64_t item = divide(r, n);
         first = item * n;
         if (item >= a.b.T) return false;
         const int seq = seq_of_row(a.b, static_cast<int>(item));
@@ -237,45 +256,44 @@ __device__ __forceinline__ bool locate_tile(const AttnArgs& a, int64_t r, AttnIt
         if (item < s.q0 || item >= s.q0 + s.n) it.n_tok = 0;
         return true;
     }
+    SeqLanes q = lanes;
     int64_t base = 0;
-    int seq = -1;
-    for (int i0 = 0; i0 < a.b.n_seqs && seq < 0; i0 += 32) {
-        const int64_t c = i0 + lane < a.b.n_seqs ? seq_tiles<TILE>(a, i0 + lane) : 0;
-        int64_t sum = c;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t up = __shfl_up_sync(0xffffffffu, sum, o);
-            if (lane >= o) sum += up;
+    for (int i0 = 0; i0 < a.b.n_seqs; i0 += 32) {
+        if (i0 > 0) q = load_lanes<TILE>(a, i0);
+        const uint32_t past = __ballot_sync(0xffffffffu, base + q.upto > r);
+        if (!past) {
+            base += __shfl_sync(0xffffffffu, q.upto, 31);
+            continue;
         }
-        const uint32_t past = __ballot_sync(0xffffffffu, base + sum > r);
-        if (past) {
-            const int l = __ffs(past) - 1;
-            seq = i0 + l;
-            base += __shfl_sync(0xffffffffu, sum - c, l);
-        } else {
-            base += __shfl_sync(0xffffffffu, sum, 31);
-        }
-    }
-    if (seq < 0) return false;
-    const SeqSpan s = load_seq(a.b, seq, a.status);
-    const int items = seq_items(a, s);
-    for (int x0 = 0; x0 < items; x0 += 32) {
-        const int c = x0 + lane < items ? item_tiles<TILE>(a, make_item(a, seq, s, x0 + lane)) : 0;
-        int sum = c;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int up = __shfl_up_sync(0xffffffffu, sum, o);
-            if (lane >= o) sum += up;
-        }
-        const uint32_t past = __ballot_sync(0xffffffffu, base + sum > r);
-        if (past) {
-            const int l = __ffs(past) - 1;
-            n = __shfl_sync(0xffffffffu, c, l);
-            first = base + __shfl_sync(0xffffffffu, sum - c, l);
-            it = make_item(a, seq, s, x0 + l);
+        const int l = __ffs(past) - 1;
+        base += __shfl_sync(0xffffffffu, q.upto - q.tiles, l);
+        const SeqSpan s{__shfl_sync(0xffffffffu, q.span.q0, l), __shfl_sync(0xffffffffu, q.span.n, l), __shfl_sync(0xffffffffu, q.span.kv, l)};
+        const int items = seq_items(a, s);
+        if (items == 1) {
+            first = base;
+            n = static_cast<int>(__shfl_sync(0xffffffffu, q.tiles, l));
+            it = make_item(a, i0 + l, s, 0);
             return true;
         }
-        base += __shfl_sync(0xffffffffu, sum, 31);
+        for (int x0 = 0; x0 < items; x0 += 32) {
+            const int c = x0 + lane < items ? item_tiles<TILE>(a, make_item(a, i0 + l, s, x0 + lane)) : 0;
+            int sum = c;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int up = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += up;
+            }
+            const uint32_t over = __ballot_sync(0xffffffffu, base + sum > r);
+            if (over) {
+                const int k = __ffs(over) - 1;
+                n = __shfl_sync(0xffffffffu, c, k);
+                first = base + __shfl_sync(0xffffffffu, sum - c, k);
+                it = make_item(a, i0 + l, s, x0 + k);
+                return true;
+            }
+            base += __shfl_sync(0xffffffffu, sum, 31);
+        }
+        return false;
     }
     return false;
 }
@@ -297,6 +315,7 @@ struct Cut {
 template <int TILE>
 struct Walk {
     int64_t per_head, share, at, end;       // share > 0: tile numbers; share 0: unit numbers
+    SeqLanes lanes;
     Cut cut;
 
     __device__ __forceinline__ void start(const AttnArgs& a)
@@ -304,9 +323,14 @@ struct Walk {
         share = 0;
         cut = Cut{0, 0, 0, 0, {0, 0, 0, 0}};
         if (a.share_min > 0) {
-            per_head = head_tiles<TILE>(a);
+            if (a.list_mode == LIST_PER_TOKEN) per_head = static_cast<int64_t>(a.b.T) * (((a.s << a.page_shift) + TILE - 1) / TILE);
+            else {
+                lanes = load_lanes<TILE>(a, 0);
+                per_head = __shfl_sync(0xffffffffu, lanes.upto, 31);
+                for (int i0 = 32; i0 < a.b.n_seqs; i0 += 32) per_head += __shfl_sync(0xffffffffu, load_lanes<TILE>(a, i0).upto, 31);
+            }
             const int64_t total = per_head * a.n_kv_heads;
-            share = max((total + a.grid - 1) / a.grid, static_cast<int64_t>(a.share_min));
+            share = max(divide(total + a.grid - 1, a.grid), static_cast<int64_t>(a.share_min));
             at = blockIdx.x * share;
             end = min(at + share, total);
         } else {
@@ -318,8 +342,8 @@ struct Walk {
     {
         while (at < end) {
             if (share == 0) {
-                g.head = static_cast<int>(at % a.n_kv_heads);
-                const bool some = attn_item(a, static_cast<int>(at / a.n_kv_heads), g.it);
+                g.head = static_cast<int>(divide(at, a.n_items));
+                const bool some = attn_item(a, static_cast<int>(at - static_cast<int64_t>(g.head) * a.n_items), g.it);
                 at += a.grid;
                 if (!some) continue;
                 g.t_lo = 0;
@@ -328,16 +352,16 @@ struct Walk {
             } else {
                 int64_t first;
                 int n;
-                g.head = static_cast<int>(at / per_head);
+                g.head = static_cast<int>(divide(at, per_head));
                 const int64_t head_at = g.head * per_head;
-                if (!locate_tile<TILE>(a, at - head_at, g.it, first, n)) return false;
+                if (!locate_tile<TILE>(a, lanes, at - head_at, g.it, first, n)) return false;
                 first += head_at;
                 g.t_lo = static_cast<int>(at - first);
                 g.t_hi = static_cast<int>(min(first + n, end) - first);
                 const bool whole = g.t_lo == 0 && g.t_hi == n;
                 g.slot = whole ? -1 : 2 * static_cast<int>(blockIdx.x) + (first + n > end ? 1 : 0);
                 if (first + n > end && first >= blockIdx.x * share)
-                    cut = Cut{g.it.tok0, g.it.n_tok, g.head, static_cast<int32_t>((first + n - 1) / share), {0, 0, 0, 0}};
+                    cut = Cut{g.it.tok0, g.it.n_tok, g.head, static_cast<int32_t>(divide(first + n - 1, share)), {0, 0, 0, 0}};
                 at = first + g.t_hi;
                 if (g.it.n_tok <= 0) continue;
             }
@@ -391,6 +415,16 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
     return false;
 }
 
+// Box of a 5-D map (column of a half, row, half, head, page): all columns of its rows, half by half.
+__device__ __forceinline__ void tma_load_rows(void* dst, const void* map, int row, int head, int page, uint64_t* bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %2, %4, %5}], [%6];" ::"r"(
+            smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(head), "r"(page), "r"(smem_u32(bar))
+        : "memory");
+}
+
 // Box of a 4-D map (column, row, head, page) into this block's shared memory; the column is 0 or 64, so every copy starts on a
 // 16-byte boundary.
 __device__ __forceinline__ void tma_load_4d(void* dst, const void* map, int c0, int c1, int c2, int c3, uint64_t* bar)
@@ -402,6 +436,22 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const void* map, int c0, 
         : "memory");
 }
 
+__device__ __forceinline__ void prefetch_map(const void* map)
+{
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+}
+// Asks for the tables and lists of a launch, spread over its blocks' producer warps, so that the dependent reads (lengths, list,
+// table, keys) do not each wait for memory.
+__device__ __forceinline__ void prefetch_tables(const AttnArgs& a)
+{
+    const int64_t line = blockIdx.x * 32 + (threadIdx.x & 31);
+    auto ask = [&](const int32_t* p, int64_t words) {
+        if (line * 32 < words) asm volatile("prefetch.global.L2 [%0];" ::"l"(p + line * 32));
+    };
+    ask(a.b.pages, (a.b.n_seqs - 1) * a.b.ld_pages + ((a.b.max_kv + a.page_size - 1) >> a.page_shift));
+    if (a.list_mode != LIST_NONE)
+        ask(a.lists, static_cast<int64_t>(a.list_mode == LIST_PER_TOKEN ? a.b.T : a.b.n_seqs) * a.list_heads * a.s);
+}
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }

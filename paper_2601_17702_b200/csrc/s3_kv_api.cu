@@ -29,19 +29,25 @@ s3_status encode_fn(EncodeTiledFn* out)
     return S3_OK;
 }
 
-// 4-D map (column, row, head, page or token) of 16-bit values; strides in elements; box 64 columns wide, 128-byte swizzle.
-s3_status make_map(unsigned char (&map)[128], s3_dtype dtype, const void* base, const uint64_t (&dims)[4], const uint64_t (&strides)[3],
-                   uint32_t box_rows, uint32_t box_last)
+// Map of 16-bit values of N dimensions, 64 columns first; strides in elements; 128-byte swizzle.
+template <int N>
+s3_status make_map(unsigned char (&map)[128], s3_dtype dtype, const void* base, const uint64_t (&dims)[N], const uint64_t (&strides)[N - 1],
+                   const uint32_t (&box)[N])
 {
     static_assert(sizeof(CUtensorMap) == 128, "a copy descriptor has 128 bytes");
     EncodeTiledFn fn;
     const s3_status st = encode_fn(&fn);
     if (st != S3_OK) return st;
-    const cuuint64_t d[4] = {dims[0], dims[1], dims[2], dims[3]};
-    const cuuint64_t s[3] = {strides[0] * 2, strides[1] * 2, strides[2] * 2};
-    const cuuint32_t box[4] = {64, box_rows, 1, box_last}, unit[4] = {1, 1, 1, 1};
+    cuuint64_t d[N], s[N - 1];
+    cuuint32_t b[N], unit[N];
+    for (int i = 0; i < N; ++i) {
+        d[i] = dims[i];
+        b[i] = box[i];
+        unit[i] = 1;
+        if (i + 1 < N) s[i] = strides[i] * 2;
+    }
     const CUresult r = fn(reinterpret_cast<CUtensorMap*>(map), dtype == S3_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
-                          4, const_cast<void*>(base), d, s, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          N, const_cast<void*>(base), d, s, b, unit, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                           CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     S3_REQUIRE(r == CUDA_SUCCESS, S3_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", static_cast<int>(r));
     return S3_OK;
@@ -106,7 +112,8 @@ s3_status make_kv_query_map(unsigned char (&map)[128], const KvCacheState& c, co
     const uint64_t D = c.d.head_dim;
     const uint64_t dims[4] = {D, static_cast<uint64_t>(group), static_cast<uint64_t>(c.d.n_kv_heads), static_cast<uint64_t>(T)};
     const uint64_t strides[3] = {D, D * group, static_cast<uint64_t>(ldq)};
-    return make_map(map, c.d.dtype, d_q, dims, strides, static_cast<uint32_t>(group), static_cast<uint32_t>(box_tokens));
+    const uint32_t box[4] = {64, static_cast<uint32_t>(group), 1, static_cast<uint32_t>(box_tokens)};
+    return make_map<4>(map, c.d.dtype, d_q, dims, strides, box);
 }
 
 }  // namespace s3
@@ -258,10 +265,16 @@ s3_status s3_kv_cache_create(s3_kv_cache** out, const s3_kv_cache_desc* desc)
     c->st.page_shift = d.page_size == 16 ? 4 : d.page_size == 32 ? 5 : d.page_size == 64 ? 6 : 7;
     c->st.box_rows = d.page_size < 64 ? d.page_size : 64;
     const uint64_t D = d.head_dim, P = d.page_size;
-    const uint64_t dims[4] = {D, P, static_cast<uint64_t>(d.n_kv_heads), static_cast<uint64_t>(d.n_pages)};
-    const uint64_t ks[3] = {D, D * P, static_cast<uint64_t>(d.k_page_stride)}, vs[3] = {D, D * P, static_cast<uint64_t>(d.v_page_stride)};
-    s3_status st = make_map(c->st.map_k, d.dtype, d.d_k, dims, ks, c->st.box_rows, 1);
-    if (st == S3_OK) st = make_map(c->st.map_v, d.dtype, d.d_v, dims, vs, c->st.box_rows, 1);
+    const uint64_t K = d.n_kv_heads, N = d.n_pages, ks = d.k_page_stride, vs = d.v_page_stride, half = 64;
+    const uint32_t rows = c->st.box_rows;
+    const uint64_t dims[4] = {D, P, K, N}, ks4[3] = {D, D * P, ks}, vs4[3] = {D, D * P, vs};
+    const uint32_t box[4] = {64, rows, 1, 1};
+    const uint64_t wide[5] = {64, P, D / 64, K, N}, ks5[4] = {D, half, D * P, ks}, vs5[4] = {D, half, D * P, vs};
+    const uint32_t wide_box[5] = {64, rows, static_cast<uint32_t>(d.head_dim / 64), 1, 1};
+    s3_status st = make_map<4>(c->st.map_k, d.dtype, d.d_k, dims, ks4, box);
+    if (st == S3_OK) st = make_map<4>(c->st.map_v, d.dtype, d.d_v, dims, vs4, box);
+    if (st == S3_OK) st = make_map<5>(c->st.wide_k, d.dtype, d.d_k, wide, ks5, wide_box);
+    if (st == S3_OK) st = make_map<5>(c->st.wide_v, d.dtype, d.d_v, wide, vs5, wide_box);
     if (st != S3_OK) {
         delete c;
         return st;
