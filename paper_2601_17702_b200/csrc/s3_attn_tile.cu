@@ -7,8 +7,8 @@
 //   warp 0       TMA producer: finds the segments, copies Q, then K and V tiles page by page into a ring of shared-memory slots
 //                (128-byte swizzle), running ahead into the next segment;
 //   warp 1       MMA issuer: one elected lane issues tcgen05.mma for S = Q K^T (both operands in shared memory) and O += P V (P read
-//                from tensor memory, V as the MN-major operand, so no transpose is ever made);
-//   warp 2       zeroes the rows of a V tile that hold no position of the sequence (a page's tail may hold anything);
+//                from tensor memory, V as the MN-major operand, so no transpose is ever made), after the warp has zeroed the rows of V
+//                that hold no position of the sequence;
 //   warps 4-7, 8-11   two softmax groups, a thread per row: S from tensor memory into registers, running maximum, exponentials,
 //                P back over S in the cache's type.
 // With two query tiles (PAIR) each group owns one and both use every key tile; with one query tile the groups take the even
@@ -46,6 +46,14 @@ struct SegInfo {
     int head, t_lo, n_tiles, v_base, slot;         // n_tiles 0: no more segments
 };
 
+// First position of each 16 keys of a tile, -1 where no block is listed; whether some of its rows hold no position of the sequence.
+// Written with the copy of the tile's keys into entry (tile mod 8): by the time an entry is written again, the tile eight before
+// has been consumed, since fewer than eight tiles fit the ring.
+struct TileWhere {
+    int pos[BN / 16];
+    int unclean, unused[7];
+};
+
 template <int D, bool PAIR>
 struct Layout {
     static constexpr int TILE_BYTES = BN * D * 2;
@@ -54,7 +62,8 @@ struct Layout {
     static constexpr int SLOTS = (D == 128 ? 7 : 10) - Q_TILES;
     static constexpr int RING = Q_BYTES;
     static constexpr int MEET = RING + SLOTS * TILE_BYTES;             // [2][128] floats: reference and sum of the odd tiles' group
-    static constexpr int BARS = MEET + 1024;
+    static constexpr int WHERE = MEET + 1024;                          // positions of the key tiles in flight, for lists
+    static constexpr int BARS = WHERE + 8 * static_cast<int>(sizeof(TileWhere));
     static constexpr int TOTAL = BARS + 512;
     static_assert(TOTAL <= 227 * 1024, "one thread block per SM");
 };
@@ -233,14 +242,13 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
     uint64_t& q_full = seg_empty[2];
     uint64_t& q_empty = seg_empty[3];
     uint64_t& o_full = seg_empty[4];
-    uint64_t& dirty_bar = seg_empty[5];
-    uint64_t& clean_bar = seg_empty[6];
-    uint64_t& meet_bar = seg_empty[7];
-    uint64_t& met_bar = seg_empty[8];
-    SegInfo* infos = reinterpret_cast<SegInfo*>(seg_empty + 9);
+    uint64_t& meet_bar = seg_empty[5];
+    uint64_t& met_bar = seg_empty[6];
+    TileWhere* where = reinterpret_cast<TileWhere*>(smem + L::WHERE);
+    SegInfo* infos = reinterpret_cast<SegInfo*>(seg_empty + 7);
     uint32_t& tmem_slot = *reinterpret_cast<uint32_t*>(infos + 2);
     volatile uint32_t* abort_flag = &tmem_slot + 1;
-    static_assert((2 * SLOTS + 19) * 8 + 2 * sizeof(SegInfo) + 8 <= 512, "barriers and descriptions fit");
+    static_assert((2 * SLOTS + 17) * 8 + 2 * sizeof(SegInfo) + 8 <= 512, "barriers and descriptions fit");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     cudaTriggerProgrammaticLaunchCompletion();       // the join's blocks may take their places; they wait for this grid's end
@@ -251,13 +259,11 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
             mbar_init(&p_half[i], 4);                                  // the group's warps
             mbar_init(&p_full[i], 4);
             mbar_init(&seg_full[i], 1);
-            mbar_init(&seg_empty[i], 10);                              // MMA warp, cleaning warp, eight softmax warps
+            mbar_init(&seg_empty[i], 9);                               // MMA warp and eight softmax warps
         }
         mbar_init(&q_full, 1);
         mbar_init(&q_empty, 1);
         mbar_init(&o_full, 1);
-        mbar_init(&dirty_bar, 1);
-        mbar_init(&clean_bar, 1);
         mbar_init(&meet_bar, 4);
         mbar_init(&met_bar, 4);
         *abort_flag = 0;
@@ -285,16 +291,12 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
         if (id < 0 || id > (it.pos_last >> a.page_shift) || ((id + 1) << a.page_shift) <= first_seen(a, it)) return -1;
         return (id << a.page_shift) + (v & (a.page_size - 1));
     };
-    // Whether the key tile at v0 has rows without a position of the sequence: their values have to be zeroed.
-    auto unclean = [&](const AttnItem& it, int head, int v0) -> bool {
-        if (a.list_mode == LIST_NONE) return v0 + BN > it.kv;
-        bool bad = false;
-        for (int u = 0; u < BN; u += 16) {
-            const int pos = pos_of(it, head, v0 + u);
-            bad |= pos < 0 || pos + 16 > it.kv;
-        }
-        return bad;
+    // Whether key tile `tile` of the block (at v0 of its segment) has rows without a position: their values have to be zeroed.
+    auto unclean = [&](const AttnItem& it, int v0, uint32_t tile) -> bool {
+        return a.list_mode == LIST_NONE ? v0 + BN > it.kv : where[tile % 8].unclean != 0;
     };
+    // First position of the u-th 16 keys of that tile.
+    auto pos_at = [&](int v0, uint32_t tile, int u) -> int { return a.list_mode == LIST_NONE ? v0 + 16 * u : where[tile % 8].pos[u]; };
     auto give_up = [&](uint32_t code) {
         dev_set_error(a.status, code);
         *abort_flag = 1;
@@ -321,6 +323,7 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
             bool some = walk.next(a, g), some_next = false;
             const int box = a.box_rows, per_tile = BN / box, group_tiles = 32 / per_tile;
             int segs = 0;
+            uint32_t first_tile = 0;                                   // of the segment, among the block's
             bool ok = true;
             auto wait = [&](uint64_t* bar, uint32_t parity) {
                 ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
@@ -364,6 +367,16 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
                     if (round > 0 && !wait(&empty_bar[st], (round - 1) & 1)) return false;
                     const bool mine = lane < per_tile && page >= 0;
                     const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, mine));
+                    if (!value && a.list_mode != LIST_NONE) {
+                        TileWhere& w = where[(first_tile + j) % 8];
+                        const int units = box / 16;
+                        const bool part = lane < per_tile && (page < 0 || pos + box > g.it.kv);
+                        const uint32_t parts = __ballot_sync(0xffffffffu, part);
+                        if (lane < per_tile)
+                            for (int u = 0; u < units; ++u) w.pos[lane * units + u] = page < 0 || pos + 16 * u >= g.it.kv ? -1 : pos + 16 * u;
+                        if (lane == 0) w.unclean = parts != 0;
+                        __syncwarp();
+                    }
                     if (lane == 0) {
                         if (boxes) mbar_expect_tx(&full_bar[st], boxes * static_cast<uint32_t>(box) * D * 2);
                         else mbar_arrive(&full_bar[st]);
@@ -392,6 +405,7 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
                     }
                 }
                 if (!ok) break;
+                first_tile += n_tiles;
                 g = g_next;
                 some = some_next;
             }
@@ -410,7 +424,8 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
                 constexpr uint32_t idesc_o = base | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17);     // V: MN-major
                 // 227 KB of shared memory: an address in 16-byte units never carries out of its 14 bits
                 const uint32_t q_desc = desc_lo(smem_u32(smem), 16), k_desc = desc_lo(smem_u32(ring), 16), v_desc = desc_lo(smem_u32(ring), BN * 128);
-                uint32_t used = 0, cleaned = 0, turns0 = 0, turns1 = 0;       // ring loads, cleaned tiles, weights taken from each group
+                uint32_t used = 0, turns0 = 0, turns1 = 0;             // ring loads, weights taken from each group
+                uint32_t tile = 0;                                     // key tiles of the block so far
                 bool ok = true;
                 auto need = [&](uint64_t* bar, uint32_t parity, uint32_t code) {
                     ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
@@ -452,13 +467,22 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
                         ++used;
                     }
                     if (ok && n_tiles <= AHEAD) commit(one, &q_empty);
-                    for (int j = 0; j < n_tiles && ok; ++j) {
+                    for (int j = 0; j < n_tiles && ok; ++j, ++tile) {
                         if (!slot_ready()) break;
                         const uint32_t sv = used % SLOTS;
                         ++used;
-                        if (__any_sync(0xffffffffu, unclean(info.it, info.head, v_lo + j * BN))) {
-                            if (lane == 0) mbar_arrive(&dirty_bar);
-                            if (!need(&clean_bar, cleaned++ & 1, DEV_TIMEOUT_ACC_EMPTY)) break;
+                        if (unclean(info.it, v_lo + j * BN, tile)) {
+                            // rows of V that hold no position may hold anything (a page's tail, an older tile): zero them
+                            unsigned char* tile_v = ring + sv * L::TILE_BYTES;
+                            for (int u = 0; u < BN / 16; ++u) {
+                                const int pos = pos_at(v_lo + j * BN, tile, u), there = pos < 0 ? 0 : min(max(info.it.kv - pos, 0), 16);
+                                for (int x = lane; x < (16 - there) * (D / 8); x += 32) {
+                                    const int row = 16 * u + there + x / (D / 8), c = x % (D / 8);
+                                    *reinterpret_cast<uint4*>(tile_v + (c >> 3) * BN * 128 + row * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+                                }
+                            }
+                            fence_async_smem();
+                            __syncwarp();
                         }
                         const bool more = j + AHEAD < n_tiles;
                         const uint32_t sk = used % SLOTS;
@@ -494,43 +518,6 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
                     if (lane == 0) mbar_arrive(&seg_empty[seg & 1]);
                 }
             }
-        } else if (warp == 2) {
-            // ---------------- values past the sequence ----------------
-            // The MMA thread hands a tile over once it has landed. V tile j of a segment is its ring load number 2j + AHEAD while
-            // key tiles still come (K_{j+AHEAD} follows V_j).
-            uint32_t at = 0, handed = 0;
-            SegInfo info;
-            for (int seg = 0;; ++seg) {
-                bool ok = __all_sync(0xffffffffu, mbar_wait(&seg_full[seg & 1], (seg >> 1) & 1, abort_flag));
-                if (!ok) break;                                        // another role has reported why
-                info = infos[seg & 1];
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&seg_empty[seg & 1]);
-                if (info.n_tiles == 0) break;
-                at += min(AHEAD, info.n_tiles);
-                for (int j = 0; j < info.n_tiles && ok; ++j) {
-                    const int v0 = info.v_base + (info.t_lo + j) * BN;
-                    if (unclean(info.it, info.head, v0)) {
-                        const uint32_t st = at % SLOTS;
-                        ok = __all_sync(0xffffffffu, mbar_wait(&dirty_bar, handed++ & 1, abort_flag));
-                        if (!ok) break;
-                        for (int u = 0; u < BN; u += 16) {
-                            const int pos = pos_of(info.it, info.head, v0 + u);
-                            const int live = pos < 0 ? 0 : min(max(info.it.kv - pos, 0), 16);
-                            for (int x = lane; x < (16 - live) * (D / 8); x += 32) {
-                                const int row = u + live + x / (D / 8), c = x % (D / 8);
-                                *reinterpret_cast<uint4*>(ring + st * L::TILE_BYTES + (c >> 3) * BN * 128 + row * 128 + (c & 7) * 16) =
-                                    make_uint4(0, 0, 0, 0);
-                            }
-                        }
-                        fence_async_smem();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&clean_bar);
-                    }
-                    at += j + AHEAD < info.n_tiles ? 2 : 1;
-                }
-                if (!ok) break;
-            }
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
@@ -542,7 +529,7 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
         const int first_tok = PAIR ? i * tile_tok : 0;                 // first token of the tile, relative to the item
         const int tok = first_tok + row / a.group, g = row % a.group;
         const f32x2 scale2 = pair_of(a.scale_log2, a.scale_log2);
-        uint32_t turn = 0;                                             // key tiles this group has taken
+        uint32_t turn = 0, tile0 = 0;                                  // key tiles this group has taken; the block's before this segment
         bool ok = true;
         for (int seg = 0;; ++seg) {
             ok = __all_sync(0xffffffffu, mbar_wait(&seg_full[seg & 1], (seg >> 1) & 1, abort_flag));
@@ -556,107 +543,100 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
             float m = -INFINITY, l = 0.0f;                             // reference of the exponentials (scaled, base 2), sum
             int turns = 0;
             for (int j = PAIR ? 0 : i; j < info.n_tiles; j += PAIR ? 1 : 2, ++turns, ++turn) {
-                const int v0 = info.v_base + (info.t_lo + j) * BN;
-                bool edge;                                             // some row may not see some key
-                if (a.list_mode == LIST_NONE) edge = v0 + BN - 1 > qlo || (a.window > 0 && v0 <= qhi - a.window);
-                else {
-                    edge = false;
-                    for (int u = 0; u < BN; u += 16) {
-                        const int pos = pos_of(info.it, info.head, v0 + u);
-                        edge |= pos < 0 || pos + 15 > qlo || (a.window > 0 && pos <= qhi - a.window);
-                    }
-                }
                 ok = __all_sync(0xffffffffu, mbar_wait(&s_full[i], turn & 1, abort_flag));
                 if (!ok) break;
                 tc_fence_after();
+                const int v0 = info.v_base + (info.t_lo + j) * BN;
+                const uint32_t tile = tile0 + j;
                 float s[4][32];
                 tm_ld32(my_s, s[0]);
+                bool look;                                             // some row may not see some key, or there is no reference yet
+                if (a.list_mode == LIST_NONE) look = v0 + BN - 1 > qlo || (a.window > 0 && v0 <= qhi - a.window);
+                else {
+                    look = false;
+#pragma unroll
+                    for (int u = 0; u < BN / 16; ++u) {
+                        const int pos = where[tile % 8].pos[u];
+                        look |= pos < 0 || pos + 15 > qlo || (a.window > 0 && pos <= qhi - a.window);
+                    }
+                }
+                const bool edge = look;
+                look |= turns == 0;
                 wait_ld();
 #pragma unroll
                 for (int c = 1; c < 4; ++c) tm_ld32(my_s + 32 * c, s[c]);
 
-                // The weights are made with the reference as it stands. Before the first half of them is handed over, its sum and the
-                // largest score of the second half, which the multiply-add pipes find meanwhile, tell whether a weight may be too
-                // large (or a score is not a number); then, on the first tile and where keys are masked, the tile is done over
-                // with its maximum looked at first.
+                // Where keys are masked, and on the first tile, the tile's maximum is looked at first. Otherwise the weights are made
+                // with the reference as it stands; before the first half of them is handed over, its sum and the largest score of
+                // the second half, which the multiply-add pipes find meanwhile, tell whether a weight may be too large (or a score
+                // is not a number), and then it is done over with the maximum looked at.
                 uint32_t p_lo[32], p_hi[32];
-                f32x2 sum[2] = {0, 0};                                 // pairs of +0
-                float ref = m == -INFINITY ? 0.0f : -m;
-                bool again = true;
-                if (!edge && turns > 0) {
-                    const f32x2 ref2 = pair_of(ref, ref);
-                    weights<T>(s[0], scale2, ref2, p_lo, sum);
-                    wait_ld();
-                    weights<T>(s[1], scale2, ref2, p_lo + 16, sum);
-                    const float a_hi = max_of(s[2]), b_hi = max_of(s[3]), top = max3(a_hi, b_hi, b_hi) * a.scale_log2;
-                    again = __any_sync(0xffffffffu, live && !(total(sum) <= 16384.0f && top <= m + CHECK_AT));
-                    if (!again) {
-                        tm_st32(my_s, p_lo);
-                        weights<T>(s[2], scale2, ref2, p_hi, sum);
-                        wait_st();
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&p_half[i]);        // one arrival per warp: 128 on one barrier take turns
-                        weights<T>(s[3], scale2, ref2, p_hi + 16, sum);
-                        tm_st32(my_s + 32, p_hi);
-                    }
-                }
-                if (again) {
-                    wait_ld();
-                    if (edge) {
+                f32x2 sum[2], ref2;
+                for (;;) {
+                    if (look) {
+                        wait_ld();
+                        if (edge) {
 #pragma unroll
-                        for (int u = 0; u < BN; u += 16) {
-                            const int pos = pos_of(info.it, info.head, v0 + u);
-                            const int hi = pos < 0 ? -1 : qpos - pos, lo = a.window > 0 ? hi - a.window : -1;      // visible: lo < c <= hi
+                            for (int u = 0; u < BN / 16; ++u) {
+                                const int pos = pos_at(v0, tile, u);
+                                const int hi = pos < 0 ? -1 : qpos - pos, lo = a.window > 0 ? hi - a.window : -1;      // visible: lo < c <= hi
 #pragma unroll
-                            for (int c = 0; c < 16; ++c)
-                                if (c > hi || c <= lo) s[u / 32][u % 32 + c] = -INFINITY;
+                                for (int c = 0; c < 16; ++c)
+                                    if (c > hi || c <= lo) s[u / 2][u % 2 * 16 + c] = -INFINITY;
+                            }
                         }
-                    }
-                    const float a_lo = max_of(s[0]), b_lo = max_of(s[1]), a_hi = max_of(s[2]), b_hi = max_of(s[3]);
-                    const float top = fmaxf(fmaxf(a_lo, b_lo), fmaxf(a_hi, b_hi)) * a.scale_log2;
-                    const bool grow = live && top > m + RESCALE_AT;
-                    if (__any_sync(0xffffffffu, grow)) {
-                        const float now = grow ? top : m;
-                        const float f = m == -INFINITY ? 0.0f : ex2(m - now);
-                        m = now;
-                        l *= f;
-                        if (turns > 0) {
+                        const float a_lo = max_of(s[0]), b_lo = max_of(s[1]), a_hi = max_of(s[2]), b_hi = max_of(s[3]);
+                        const float top = fmaxf(fmaxf(a_lo, b_lo), fmaxf(a_hi, b_hi)) * a.scale_log2;
+                        const bool grow = live && top > m + RESCALE_AT;
+                        if (__any_sync(0xffffffffu, grow)) {
+                            const float now = grow ? top : m;
+                            const float f = m == -INFINITY ? 0.0f : ex2(m - now);
+                            m = now;
+                            l *= f;
+                            if (turns > 0) {
 #pragma unroll
-                            for (int c = 0; c < D; c += 16) {          // narrow steps: the scores stay in registers meanwhile
-                                float o[16];
-                                tm_ld16(my_o + c, o);
-                                wait_ld();
+                                for (int c = 0; c < D; c += 16) {      // narrow steps: the scores stay in registers meanwhile
+                                    float o[16];
+                                    tm_ld16(my_o + c, o);
+                                    wait_ld();
 #pragma unroll
-                                for (int x = 0; x < 16; ++x) o[x] *= f;
-                                tm_st16(my_o + c, o);
+                                    for (int x = 0; x < 16; ++x) o[x] *= f;
+                                    tm_st16(my_o + c, o);
+                                }
                             }
                         }
                     }
-                    ref = m == -INFINITY ? 0.0f : -m;
-                    const f32x2 ref2 = pair_of(ref, ref);
-                    sum[0] = sum[1] = 0;
+                    const float ref = m == -INFINITY ? 0.0f : -m;
+                    ref2 = pair_of(ref, ref);
+                    sum[0] = sum[1] = 0;                               // pairs of +0
                     weights<T>(s[0], scale2, ref2, p_lo, sum);
+                    wait_ld();
                     weights<T>(s[1], scale2, ref2, p_lo + 16, sum);
-                    tm_st32(my_s, p_lo);
-                    weights<T>(s[2], scale2, ref2, p_hi, sum);
-                    weights<T>(s[3], scale2, ref2, p_hi + 16, sum);
-                    tm_st32(my_s + 32, p_hi);
-                    // the first product of a segment overwrites the odd group's accumulator, which the even group may still be reading
-                    if (!PAIR && i == 1 && turns == 0 && seg > 0) {
-                        ok = __all_sync(0xffffffffu, mbar_wait(&met_bar, (seg - 1) & 1, abort_flag));
-                        if (!ok) break;
-                    }
+                    if (look) break;
+                    const float a_hi = max_of(s[2]), b_hi = max_of(s[3]), top = max3(a_hi, b_hi, b_hi) * a.scale_log2;
+                    look = __any_sync(0xffffffffu, live && !(total(sum) <= 16384.0f && top <= m + CHECK_AT));
+                    if (!look) break;
                 }
+                tm_st32(my_s, p_lo);
+                weights<T>(s[2], scale2, ref2, p_hi, sum);
+                wait_st();
+                // the first product of a segment overwrites the odd group's accumulator, which the even group may still be reading
+                if (!PAIR && i == 1 && turns == 0 && seg > 0) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(&met_bar, (seg - 1) & 1, abort_flag));
+                    if (!ok) break;
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_half[i]);                // one arrival per warp: 128 on one barrier take turns
+                weights<T>(s[3], scale2, ref2, p_hi + 16, sum);
+                tm_st32(my_s + 32, p_hi);
                 wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) {
-                    if (again) mbar_arrive(&p_half[i]);
-                    mbar_arrive(&p_full[i]);
-                }
+                if (lane == 0) mbar_arrive(&p_full[i]);
                 l += total(sum);
             }
+            tile0 += info.n_tiles;
             // ---------------- results ----------------
             if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&o_full, seg & 1, abort_flag));
             if (ok && !PAIR) {
