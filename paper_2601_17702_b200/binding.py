@@ -890,14 +890,33 @@ def s3_block_select(cache: KvCache, batch: KvBatch, q: torch.Tensor, s: int, ws:
 
 def _attention_rows(cache, batch, q, out, lse, want_lse):
     assert batch.max_kv <= batch.blocks * cache.page_size
-    ldq = _rows(q, cache, batch.T)
+    T = batch.T
+    ldq, H = _rows(q, cache, T), q.shape[1]
     if out is None:
-        out = torch.empty_like(q)
-    ld_out = _rows(out, cache, batch.T, q.shape[1])
-    if lse is None and want_lse:
-        lse = q.new_empty(q.shape[:2], dtype=torch.float32)
-    assert lse is None or (lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == q.shape[:2])
-    return ldq, out, ld_out, lse
+        out = torch.empty_like(q)                        # heads stay contiguous
+        ld_out = out.stride(0) if T > 1 else H * cache.head_dim
+    else:
+        ld_out = _rows(out, cache, T, H)
+    if lse is not None:
+        assert lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and tuple(lse.shape) == (T, H)
+        return ldq, H, out, ld_out, lse, lse.data_ptr()
+    if not want_lse:
+        return ldq, H, out, ld_out, None, None
+    lse = q.new_empty((T, H), dtype=torch.float32)
+    return ldq, H, out, ld_out, lse, lse.data_ptr()
+
+
+_attn_params: dict = {}
+
+
+def _attn_ref(cache, scale, causal, window):
+    key = (cache.head_dim ** -0.5 if scale is None else scale, bool(causal), window)
+    p = _attn_params.get(key)
+    if p is None:
+        if len(_attn_params) > 256:
+            _attn_params.clear()
+        p = _attn_params[key] = C.byref(AttnParams(key[0], int(key[1]), window, 0))
+    return p
 
 
 def s3_paged_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, ws: torch.Tensor, scale: float | None = None, causal: bool = True,
@@ -905,10 +924,9 @@ def s3_paged_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, ws: torc
                        stream=None):
     """Attention of the new tokens' rotated queries q [T, n_heads, head_dim] over the cache (their keys appended before). Returns
     (out like q, lse fp32 [T, n_heads] or None). scale defaults to head_dim ** -0.5."""
-    ldq, out, ld_out, lse = _attention_rows(cache, batch, q, out, lse, want_lse)
-    params = AttnParams(cache.head_dim ** -0.5 if scale is None else scale, int(causal), window, 0)
-    _check(lib().s3_paged_attention(cache.handle, batch.ref, q.data_ptr(), ldq, q.shape[1], C.byref(params), out.data_ptr(), ld_out,
-                                    None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(stream)))
+    ldq, H, out, ld_out, lse, lse_ptr = _attention_rows(cache, batch, q, out, lse, want_lse)
+    _check(lib().s3_paged_attention(cache.handle, batch.ref, q.data_ptr(), ldq, H, _attn_ref(cache, scale, causal, window), out.data_ptr(), ld_out,
+                                    lse_ptr, ws.data_ptr(), ws.numel(), _raw_stream(stream)))
     return out, lse
 
 
@@ -917,11 +935,10 @@ def s3_block_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, blocks: 
                        lse: torch.Tensor | None = None, want_lse: bool = False, stream=None):
     """The same over listed blocks: blocks int32 [T, n_kv_heads or 1, s] (per_token; e.g. s3_block_select) or
     [n_seqs, n_kv_heads or 1, s] (one list per sequence; e.g. the top spans of s3_coactivation_score_topspans, unsqueezed)."""
-    ldq, out, ld_out, lse = _attention_rows(cache, batch, q, out, lse, want_lse)
-    assert blocks.is_cuda and blocks.dtype == torch.int32 and blocks.is_contiguous() and blocks.dim() == 3
-    assert blocks.shape[0] == (batch.T if per_token else batch.n_seqs)
-    params = AttnParams(cache.head_dim ** -0.5 if scale is None else scale, int(causal), window, 0)
-    _check(lib().s3_block_attention(cache.handle, batch.ref, q.data_ptr(), ldq, q.shape[1], blocks.data_ptr(), blocks.shape[2],
-                                    blocks.shape[1], int(per_token), C.byref(params), out.data_ptr(), ld_out,
-                                    None if lse is None else lse.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(stream)))
+    ldq, H, out, ld_out, lse, lse_ptr = _attention_rows(cache, batch, q, out, lse, want_lse)
+    n, heads, s = blocks.shape
+    assert blocks.is_cuda and blocks.dtype == torch.int32 and blocks.is_contiguous() and n == (batch.T if per_token else batch.n_seqs)
+    _check(lib().s3_block_attention(cache.handle, batch.ref, q.data_ptr(), ldq, H, blocks.data_ptr(), s, heads, int(per_token),
+                                    _attn_ref(cache, scale, causal, window), out.data_ptr(), ld_out, lse_ptr, ws.data_ptr(), ws.numel(),
+                                    _raw_stream(stream)))
     return out, lse

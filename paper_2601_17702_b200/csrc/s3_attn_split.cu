@@ -130,6 +130,7 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
         }
         Walk<TILE> walk;
         Segment g;
+        cudaGridDependencySynchronize();
         walk.start(a);
         // A lane per box: the lanes read the table entries of the next 32 boxes together, one group ahead of the copies, so that
         // no copy waits for its page number. The next segment is looked up while the ring is full.
@@ -231,6 +232,7 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
         }
     } else {
         // ---------------- compute ----------------
+        cudaGridDependencySynchronize();                              // it writes where the kernel before may still read
         __syncthreads();
         const int quad = lane & 3, r8 = lane >> 2;                    // this thread's query rows: 2 quad, 2 quad + 1 (+ 8 nt)
         const int mi = lane >> 3, mr = lane & 7;
@@ -488,6 +490,7 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ AttnA
 {
     __shared__ float acc[MANY_ROWS ? 1 : 4][D], acc_l[4];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    cudaTriggerProgrammaticLaunchCompletion();
     cudaGridDependencySynchronize();
     const Cut cut = reinterpret_cast<const Cut*>(a.cuts)[blockIdx.x];
     const int c0 = blockIdx.x, c1 = cut.last, rows = cut.n_tok * a.group;
@@ -551,9 +554,7 @@ s3_status launch_split(const KvCacheState& c, const AttnArgs& a, cudaStream_t st
     Maps maps;
     memcpy(maps.k, c.wide_k, sizeof(maps.k));
     memcpy(maps.v, c.wide_v, sizeof(maps.v));
-    split_kernel<T, D, NT><<<a.grid, THREADS, L::TOTAL, stream>>>(maps, a);
-    S3_CUDA_TRY(cudaGetLastError());
-    return S3_OK;
+    return launch_overlapped(split_kernel<T, D, NT>, dim3(a.grid), THREADS, L::TOTAL, stream, maps, a);
 }
 
 template <class T, int D>
@@ -566,19 +567,9 @@ s3_status launch_rows(const KvCacheState& c, const AttnArgs& a, cudaStream_t str
 template <class T, int D>
 s3_status launch_join_typed(const AttnArgs& a, bool tile, cudaStream_t stream)
 {
-    cudaLaunchConfig_t cfg = {};
     const int most = min(a.rows_cap, (a.list_mode == LIST_PER_TOKEN ? 1 : min(a.b.max_q, a.rows_cap)) * a.group);     // rows of an item
-    cfg.gridDim = dim3(static_cast<unsigned>(a.grid - 1), static_cast<unsigned>(tile ? (most + 7) / 8 : most));
-    cfg.blockDim = dim3(128);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;      // its launch overlaps the kernel before it
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    if (tile) S3_CUDA_TRY(cudaLaunchKernelEx(&cfg, join_kernel<T, D, true>, a));
-    else S3_CUDA_TRY(cudaLaunchKernelEx(&cfg, join_kernel<T, D, false>, a));
-    return S3_OK;
+    const dim3 grid(static_cast<unsigned>(a.grid - 1), static_cast<unsigned>(tile ? (most + 7) / 8 : most));
+    return tile ? launch_overlapped(join_kernel<T, D, true>, grid, 128, 0, stream, a) : launch_overlapped(join_kernel<T, D, false>, grid, 128, 0, stream, a);
 }
 
 }  // namespace

@@ -273,6 +273,7 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(TMEM_COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    cudaGridDependencySynchronize();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -759,9 +760,7 @@ s3_status launch_tile(const KvCacheState& c, const AttnArgs& a, cudaStream_t str
     const int tile_tok = BM / a.group < a.tok_per_item ? BM / a.group : a.tok_per_item;
     s3_status st = make_kv_query_map(maps.q, c, a.q, a.ldq, a.b.T, a.group, tile_tok);
     if (st != S3_OK) return st;
-    tile_kernel<T, D, PAIR><<<a.grid, THREADS, L::TOTAL, stream>>>(maps, a);
-    S3_CUDA_TRY(cudaGetLastError());
-    return S3_OK;
+    return launch_overlapped(tile_kernel<T, D, PAIR>, dim3(a.grid), THREADS, L::TOTAL, stream, maps, a);
 }
 
 template <class T, int D>

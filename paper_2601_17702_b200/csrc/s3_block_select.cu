@@ -168,6 +168,8 @@ __global__ void __launch_bounds__(THREADS, TT == 16 ? 5 : 2) select_kernel(const
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int head = blockIdx.x % a.n_kv_heads, item = blockIdx.x / a.n_kv_heads;
     int seq = item, idx = 0;
+    cudaTriggerProgrammaticLaunchCompletion();
+    cudaGridDependencySynchronize();
     if (!a.one_item_per_seq) {
         const KvBatchDev& b = a.b;
         if (!locate_item(b.n_seqs, item, [&](int i) { return (load_seq(b, i, nullptr).n + TT - 1) / TT; }, seq, idx)) return;
@@ -292,9 +294,7 @@ s3_status launch_one(SelectArgs& a, cudaStream_t stream)
     a.one_item_per_seq = a.b.max_q <= TT;
     const int64_t items = a.one_item_per_seq ? a.b.n_seqs : static_cast<int64_t>(a.b.T) / TT + a.b.n_seqs;
     S3_REQUIRE(items * a.n_kv_heads < (int64_t(1) << 31), S3_ERR_UNSUPPORTED, "the batch needs too many thread blocks");
-    select_kernel<T, D, TT, THREADS><<<static_cast<unsigned>(items * a.n_kv_heads), THREADS, smem, stream>>>(a);
-    S3_CUDA_TRY(cudaGetLastError());
-    return S3_OK;
+    return launch_overlapped(select_kernel<T, D, TT, THREADS>, dim3(static_cast<unsigned>(items * a.n_kv_heads)), THREADS, smem, stream, a);
 }
 
 template <class T, int D>

@@ -6,12 +6,34 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <utility>
+
 #include "s3_common.cuh"
 
 namespace s3 {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kSumSteps = 4096.0f, kSumLimit = 2047.0f;   // fixed point of the summaries and of the summed queries
+
+// Launch that may begin while the kernel before it in the stream ends (programmatic launch): its blocks set themselves up, and
+// cudaGridDependencySynchronize() in the kernel waits for that kernel's end before anything it may have written is read, or
+// anything it may still read is written. Worth about a microsecond per call where calls are short.
+template <class... Params, class... Args>
+inline s3_status launch_overlapped(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t stream, Args&&... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    S3_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...));
+    return S3_OK;
+}
 
 struct KvCacheState {
     s3_kv_cache_desc d;

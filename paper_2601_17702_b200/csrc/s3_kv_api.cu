@@ -63,6 +63,28 @@ struct AttnPlan {
     int grid, share_min, rows_cap;
 };
 
+// Chooses whole units or shares for a plan whose items are set, and returns the modelled time in key tiles. tile_cost: time of one of
+// this plan's key tiles; extra: what shares cost beside their tiles (second launch, partial results, segments cut short).
+double choose_shares(AttnPlan& p, const s3_kv_batch& b, int n_kv_heads, int list_mode, int64_t keys, double tile_cost, double extra)
+{
+    const int64_t places = (p.tile ? 1 : 2) * static_cast<int64_t>(device_sm_count());     // thread blocks that run at a time
+    const int64_t units = static_cast<int64_t>(p.n_items) * n_kv_heads, tiles = (keys + (p.tile ? 127 : 63)) / (p.tile ? 128 : 64);
+    // Lists and the items of one sequence are alike: whole units take whole rounds. Sequences of a batch may have any length up to
+    // max_kv, which the host does not see: on average taken as 0.6 of it, and whole units end with the longest.
+    const bool alike = list_mode != LIST_NONE || b.n_seqs == 1;
+    const int64_t rounds = (units + places - 1) / places;
+    const double whole = alike || rounds <= 1 ? static_cast<double>(rounds * tiles) * tile_cost : 1e30;
+    const double share = (alike ? 1.0 : 0.6) * static_cast<double>(units) * tiles / places * tile_cost + extra;
+    if (whole <= share) {
+        p.grid = static_cast<int>(units < places ? units : places);
+        p.share_min = 0;
+        return whole;
+    }
+    p.grid = static_cast<int>(places);
+    p.share_min = p.tile ? 2 : 4;
+    return share;
+}
+
 // keys: the most virtual keys an item can have.
 AttnPlan plan_attention(const s3_kv_batch& b, int group, int n_kv_heads, int list_mode, int64_t keys)
 {
@@ -72,28 +94,26 @@ AttnPlan plan_attention(const s3_kv_batch& b, int group, int n_kv_heads, int lis
         p.tok_per_item = 1;
         p.n_items = b.T;
         p.one_item_per_seq = 0;
+        choose_shares(p, b, n_kv_heads, list_mode, keys, 1.0, p.tile ? 6.0 : 12.0);
     } else {
         p.tile = static_cast<int64_t>(b.max_q) * group > kSplitRows;
         const int one = (p.tile ? kTileRows : kSplitRows) / group;
-        p.tok_per_item = p.tile && b.max_q > one ? 2 * one : one;
-        p.one_item_per_seq = b.max_q <= p.tok_per_item;
-        p.n_items = p.one_item_per_seq ? b.n_seqs : b.T / p.tok_per_item + b.n_seqs;
+        auto items = [&](AttnPlan& q, int tokens) {
+            q.tok_per_item = tokens;
+            q.one_item_per_seq = b.max_q <= tokens;
+            q.n_items = q.one_item_per_seq ? b.n_seqs : b.n_seqs == 1 ? (b.T + tokens - 1) / tokens : b.T / tokens + b.n_seqs;
+        };
+        items(p, one);
+        // With one query tile per item the two softmax groups share the keys: a key tile takes a little more than half the time that it
+        // takes with two, there are twice as many units, and every key is copied twice as often.
+        const double single = choose_shares(p, b, n_kv_heads, list_mode, keys, p.tile ? 0.6 : 1.0, p.tile ? 6.0 : 12.0);
+        if (p.tile && b.max_q > one) {
+            AttnPlan q = p;
+            items(q, 2 * one);
+            if (choose_shares(q, b, n_kv_heads, list_mode, keys, 1.0, 6.0) <= single) p = q;
+        }
     }
-    p.rows_cap = !p.tile ? kSplitRows : p.tok_per_item * group;
-    const int64_t places = (p.tile ? 1 : 2) * static_cast<int64_t>(device_sm_count());     // thread blocks that run at a time
-    const int64_t units = static_cast<int64_t>(p.n_items) * n_kv_heads, tiles = (keys + (p.tile ? 127 : 63)) / (p.tile ? 128 : 64);
-    // Shares end together whatever the lengths are, but cost a second launch and the partial results: about 6 tiles' time in the tile
-    // kernel, 12 in the split kernel. Units that are alike (lists; one sequence) stay whole where their rounds cost no more than
-    // that; units of several sequences, whose lengths the host does not see, when even the longest is short.
-    const int64_t extra = p.tile ? 6 : 12, rounds = (units + places - 1) / places;
-    const bool alike = list_mode != LIST_NONE || b.n_seqs == 1;
-    if (alike ? rounds * tiles <= units * tiles / places + extra : units <= places && tiles <= extra) {
-        p.grid = static_cast<int>(units < places ? units : places);
-        p.share_min = 0;
-    } else {
-        p.grid = static_cast<int>(places);
-        p.share_min = p.tile ? 2 : 4;
-    }
+    p.rows_cap = p.tile ? p.tok_per_item * group : kSplitRows;
     return p;
 }
 
@@ -294,8 +314,14 @@ size_t s3_kv_workspace_bytes(const s3_kv_cache* cache, const s3_kv_batch* batch,
     if (check_batch(cache, batch) != S3_OK || check_heads(cache, n_heads) != S3_OK) return 0;
     size_t most = 0;
     if (batch->T > 0 && batch->n_seqs > 0)
-        for (int mode = LIST_NONE; mode <= LIST_PER_SEQ; ++mode) {
-            const AttnPlan p = plan_attention(*batch, n_heads / cache->st.d.n_kv_heads, cache->st.d.n_kv_heads, mode, INT32_MAX);
+        // every call uses at most one of these: the tile kernel's pieces of two query tiles or one, the split kernel's
+        for (int tile = 0; tile < 2; ++tile) {
+            AttnPlan p;
+            p.grid = (tile ? 1 : 2) * device_sm_count();
+            p.share_min = 1;
+            const int group = n_heads / cache->st.d.n_kv_heads, one = kTileRows / group;
+            if (tile && static_cast<int64_t>(batch->max_q) * group <= kSplitRows && group <= kSplitRows) continue;
+            p.rows_cap = tile ? (batch->max_q > one ? 2 * one : one) * group : kSplitRows;
             const size_t bytes = partial_bytes(p, cache->st.d.head_dim);
             if (bytes > most) most = bytes;
         }

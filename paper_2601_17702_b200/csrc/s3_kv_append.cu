@@ -125,6 +125,8 @@ __global__ void __launch_bounds__(THREADS, 8) append_kernel(const AppendArgs a)
     int e0, e1;
     bool turn;
     pair_of(a, p, e0, e1, turn);
+    cudaTriggerProgrammaticLaunchCompletion();
+    cudaGridDependencySynchronize();
 
     if (static_cast<int>(blockIdx.x) >= a.n_kv_blocks) {
         // ---------------- queries ----------------
@@ -286,15 +288,11 @@ s3_status launch_kv_append(const KvCacheState& c, const KvBatchDev& b, const s3_
     a.n_kv_blocks = static_cast<int>(kv_blocks);
     const dim3 grid(static_cast<unsigned>(kv_blocks + q_blocks));
     const bool wide = c.d.head_dim == 128;
-    if (c.d.dtype == S3_BF16) {
-        if (wide) append_kernel<__nv_bfloat16, 128><<<grid, THREADS, 0, stream>>>(a);
-        else append_kernel<__nv_bfloat16, 64><<<grid, THREADS, 0, stream>>>(a);
-    } else {
-        if (wide) append_kernel<__half, 128><<<grid, THREADS, 0, stream>>>(a);
-        else append_kernel<__half, 64><<<grid, THREADS, 0, stream>>>(a);
-    }
-    S3_CUDA_TRY(cudaGetLastError());
-    return S3_OK;
+    if (c.d.dtype == S3_BF16)
+        return wide ? launch_overlapped(append_kernel<__nv_bfloat16, 128>, grid, THREADS, 0, stream, a)
+                    : launch_overlapped(append_kernel<__nv_bfloat16, 64>, grid, THREADS, 0, stream, a);
+    return wide ? launch_overlapped(append_kernel<__half, 128>, grid, THREADS, 0, stream, a)
+                : launch_overlapped(append_kernel<__half, 64>, grid, THREADS, 0, stream, a);
 }
 
 }  // namespace s3
