@@ -138,7 +138,7 @@ struct AttnArgs {
     float* part_o;              // [2 * grid][rows_cap][head_dim]
     float* part_lse;            // [2 * grid][rows_cap], base 2
     int32_t* cuts;              // [grid][8]: the unit that the cut behind a block's share divides first, see Cut
-    int32_t grid, share_min, rows_cap, tok_per_item, n_items, one_item_per_seq;
+    int32_t grid, share_min, whole_rounds, rows_cap, tok_per_item, n_items, one_item_per_seq;
     uint32_t* status;
 };
 
@@ -337,6 +337,8 @@ struct Cut {
 template <int TILE>
 struct Walk {
     int64_t per_head, share, at, end;       // share > 0: tile numbers; share 0: unit numbers
+    int64_t unit, unit_end;                 // share > 0: units of the whole rounds before the shares
+    int64_t origin;                         // and the tile number where the shares begin
     SeqLanes lanes;
     Cut cut;
 
@@ -352,8 +354,21 @@ struct Walk {
                 for (int i0 = 32; i0 < a.b.n_seqs; i0 += 32) per_head += __shfl_sync(0xffffffffu, load_lanes<TILE>(a, i0).upto, 31);
             }
             const int64_t total = per_head * a.n_kv_heads;
-            share = max(divide(total + a.grid - 1, a.grid), static_cast<int64_t>(a.share_min));
-            at = blockIdx.x * share;
+            unit = blockIdx.x;
+            unit_end = static_cast<int64_t>(a.whole_rounds) * a.grid;
+            origin = 0;
+            if (unit_end > 0) {                                       // one sequence: its items before the first that is shared
+                const int64_t head = divide(unit_end, a.n_items);
+                const SeqSpan s{__shfl_sync(0xffffffffu, lanes.span.q0, 0), __shfl_sync(0xffffffffu, lanes.span.n, 0), __shfl_sync(0xffffffffu, lanes.span.kv, 0)};
+                const int before = min(static_cast<int>(unit_end - head * a.n_items), seq_items(a, s));
+                int64_t sum = 0;
+                for (int x = threadIdx.x & 31; x < before; x += 32) sum += item_tiles<TILE>(a, make_item(a, 0, s, x));
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                origin = head * per_head + sum;
+            }
+            share = max(divide(max(total - origin, int64_t(0)) + a.grid - 1, a.grid), static_cast<int64_t>(a.share_min));
+            at = origin + blockIdx.x * share;
             end = min(at + share, total);
         } else {
             at = blockIdx.x;
@@ -362,6 +377,17 @@ struct Walk {
     }
     __device__ __forceinline__ bool next(const AttnArgs& a, Segment& g)
     {
+        while (share > 0 && unit < unit_end) {
+            g.head = static_cast<int>(divide(unit, a.n_items));
+            const bool some = attn_item(a, static_cast<int>(unit - static_cast<int64_t>(g.head) * a.n_items), g.it);
+            unit += a.grid;
+            if (!some) continue;
+            g.t_lo = 0;
+            g.t_hi = item_tiles<TILE>(a, g.it);
+            g.slot = -1;
+            g.v_base = a.list_mode == LIST_NONE ? first_seen(a, g.it) & ~(TILE - 1) : 0;
+            return true;
+        }
         while (at < end) {
             if (share == 0) {
                 g.head = static_cast<int>(divide(at, a.n_items));
@@ -382,8 +408,8 @@ struct Walk {
                 g.t_hi = static_cast<int>(min(first + n, end) - first);
                 const bool whole = g.t_lo == 0 && g.t_hi == n;
                 g.slot = whole ? -1 : 2 * static_cast<int>(blockIdx.x) + (first + n > end ? 1 : 0);
-                if (first + n > end && first >= blockIdx.x * share)
-                    cut = Cut{g.it.tok0, g.it.n_tok, g.head, static_cast<int32_t>(divide(first + n - 1, share)), {0, 0, 0, 0}};
+                if (first + n > end && first >= origin + blockIdx.x * share)
+                    cut = Cut{g.it.tok0, g.it.n_tok, g.head, static_cast<int32_t>(divide(first + n - 1 - origin, share)), {0, 0, 0, 0}};
                 at = first + g.t_hi;
                 if (g.it.n_tok <= 0) continue;
             }

@@ -60,7 +60,7 @@ constexpr int kTileRows = 128;
 struct AttnPlan {
     bool tile;                             // tile kernel, else split kernel
     int tok_per_item, n_items, one_item_per_seq;
-    int grid, share_min, rows_cap;
+    int grid, share_min, whole_rounds, rows_cap;
 };
 
 // Chooses whole units or shares for a plan whose items are set, and returns the modelled time in key tiles. tile_cost: time of one of
@@ -75,6 +75,7 @@ double choose_shares(AttnPlan& p, const s3_kv_batch& b, int n_kv_heads, int list
     const int64_t rounds = (units + places - 1) / places;
     const double whole = alike || rounds <= 1 ? static_cast<double>(rounds * tiles) * tile_cost : 1e30;
     const double share = (alike ? 1.0 : 0.6) * static_cast<double>(units) * tiles / places * tile_cost + extra;
+    p.whole_rounds = 0;
     if (whole <= share) {
         p.grid = static_cast<int>(units < places ? units : places);
         p.share_min = 0;
@@ -82,6 +83,9 @@ double choose_shares(AttnPlan& p, const s3_kv_batch& b, int n_kv_heads, int list
     }
     p.grid = static_cast<int>(places);
     p.share_min = p.tile ? 2 : 4;
+    // A chunk late in a prompt: units of nearly equal length. Whole rounds of them go first, all blocks sweeping the keys in step, and
+    // only the rest is shared: the blocks of a key head then read the same tiles at the same time.
+    if (p.tile && list_mode == LIST_NONE && b.n_seqs == 1 && b.max_kv >= 4 * static_cast<int64_t>(b.max_q)) p.whole_rounds = static_cast<int>(units / places);
     return share;
 }
 
@@ -237,6 +241,7 @@ s3_status attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const vo
 
     a.grid = p.grid;
     a.share_min = p.share_min;
+    a.whole_rounds = p.whole_rounds;
     a.rows_cap = p.rows_cap;
     const size_t need = 256 + partial_bytes(p, c.d.head_dim);
     S3_REQUIRE(p.share_min == 0 || ws_bytes >= need, S3_ERR_CAPACITY, "workspace holds %zu bytes, %zu needed", ws_bytes, need);
