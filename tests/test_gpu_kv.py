@@ -496,3 +496,78 @@ def test_refusals():
     s = R.Setup([(1, 4000)], 8, 2, 128, 16, seed=1)
     d = Device(s)
     refused(S.S3_ERR_CAPACITY, S.s3_paged_attention, d.cache, d.batch, d.q, d.ws[:512])
+
+
+def on_gpu(s, blocks=None):
+    """The 64-bit definition for one long sequence, on the GPU a key head at a time."""
+    (n, kv), G = s.lens[0], s.H // s.K
+    j, pos = torch.arange(kv, device="cuda"), torch.arange(kv - n, kv, device="cuda")[:, None]
+    out, lse = torch.zeros((n, s.H, s.D), dtype=torch.float64), torch.zeros((n, s.H), dtype=torch.float64)
+    for h in range(s.K):
+        k, v = s.held(0, h, "k").cuda(), s.held(0, h, "v").cuda()
+        for g in range(h * G, h * G + G):
+            x = (dev(s.q[:, g]).double() @ k.T * s.scale).masked_fill(j > pos, -math.inf)
+            lse[:, g] = torch.logsumexp(x, -1).cpu()
+            out[:, g] = (torch.softmax(x, -1) @ v).cpu()
+    return out, lse
+
+
+@pytest.mark.parametrize("n,kv,H,K", [(1300, 5300, 32, 8), (1290, 9001, 28, 4)])
+def test_a_chunk_late_in_a_prompt(n, kv, H, K):
+    """Enough units for whole rounds before the shares, and cuts within units."""
+    s = R.Setup([(n, kv)], H, K, 128, 64, seed=n)
+    d = Device(s)
+    out, lse = S.s3_paged_attention(d.cache, d.batch, d.q, d.ws, want_lse=True)
+    d.fine()
+    check(s, out, lse, *on_gpu(s))
+
+
+@pytest.mark.parametrize("bound", [0, 3000])
+def test_more_sequences_than_lanes(bound):
+    """Batches of over 32 and over 64 sequences, empty ones among them; max_q and max_kv may be loose bounds."""
+    for new in ([1] * 75, [(i * 7) % 41 for i in range(70)]):
+        lens = [(q, q + (i * 37) % 300) for i, q in enumerate(new)]
+        s = R.Setup(lens, 8, 2, 64, 16, seed=len(lens))
+        s.max_kv += bound
+        s.max_q = min(s.T, s.max_q + bound)
+        wide = torch.full((len(lens), s.max_kv // 16 + s.cols), -7, dtype=torch.int32)
+        wide[:, :s.cols] = s.pages
+        s.pages, s.cols = wide, wide.shape[1]
+        code, scale = summaries_of(s)
+        d = Device(s, code, scale)
+        out, lse = S.s3_paged_attention(d.cache, d.batch, d.q, d.ws, want_lse=True)
+        d.fine()
+        check(s, out, lse, *R.attention(s))
+        blocks = S.s3_block_select(d.cache, d.batch, d.q, 5, d.ws)
+        d.fine()
+        assert torch.equal(blocks.cpu(), R.select(s, code, scale, 5, 1, 2))
+        out, lse = S.s3_block_attention(d.cache, d.batch, d.q, blocks, d.ws, want_lse=True)
+        d.fine()
+        check(s, out, lse, *R.attention(s, blocks=blocks.cpu()))
+        S.s3_kv_append(d.cache, d.batch, dev(s.k), dev(s.v), d.ws)
+        d.fine()
+        for t, i, pos in s.rows():
+            assert torch.equal(d.k[int(s.pages[i, pos // 16]), :, pos % 16].cpu(), s.k[t])
+
+
+def test_a_workspace_serves_smaller_batches():
+    s = R.Setup([(300, 4000)], 16, 2, 128, 64, seed=3)
+    d = Device(s)
+    last = S.s3_kv_workspace_bytes(d.cache, d.batch, 16)
+    for T, q, kv in ((300, 300, 4000), (299, 40, 3000), (64, 17, 500), (40, 3, 500), (9, 1, 64), (1, 1, 1)):
+        b = S.KvBatch(d.batch.cu_q, d.batch.kv_len, d.batch.pages, T, q, kv)
+        now = S.s3_kv_workspace_bytes(d.cache, b, 16)
+        assert 0 < now <= last
+        last = now
+
+
+def test_example_runs_them_together():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "evidence_attention.py")
+    spec = importlib.util.spec_from_file_location("evidence_attention", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    question, answer, found = m.run(context=4096, chunk=1024)
+    # the stretch asked about is one page of 64, and holds nearly all of the attention's weight
+    assert found and question > 0.9 and min(answer) > 0.9
