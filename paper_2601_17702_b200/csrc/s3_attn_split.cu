@@ -544,13 +544,8 @@ template <class T, int D, int NT>
 s3_status launch_split(const KvCacheState& c, const AttnArgs& a, cudaStream_t stream)
 {
     using L = Layout<D, NT>;
-    static bool raised[64] = {};                 // the attribute is kept per device; setting it twice does no harm
-    int dev = 0;
-    S3_CUDA_TRY(cudaGetDevice(&dev));
-    if (dev >= 64 || !raised[dev]) {
-        S3_CUDA_TRY(cudaFuncSetAttribute(split_kernel<T, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::TOTAL));
-        if (dev < 64) raised[dev] = true;
-    }
+    const s3_status allowed = allow_smem<split_kernel<T, D, NT>>(L::TOTAL);
+    if (allowed != S3_OK) return allowed;
     Maps maps;
     memcpy(maps.k, c.wide_k, sizeof(maps.k));
     memcpy(maps.v, c.wide_v, sizeof(maps.v));

@@ -747,13 +747,8 @@ template <class T, int D, bool PAIR>
 s3_status launch_tile(const KvCacheState& c, const AttnArgs& a, cudaStream_t stream)
 {
     using L = Layout<D, PAIR>;
-    static bool raised[64] = {};                 // the attribute is kept per device; setting it twice does no harm
-    int dev = 0;
-    S3_CUDA_TRY(cudaGetDevice(&dev));
-    if (dev >= 64 || !raised[dev]) {
-        S3_CUDA_TRY(cudaFuncSetAttribute(tile_kernel<T, D, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::TOTAL));
-        if (dev < 64) raised[dev] = true;
-    }
+    const s3_status allowed = allow_smem<tile_kernel<T, D, PAIR>>(L::TOTAL);
+    if (allowed != S3_OK) return allowed;
     Maps maps;
     memcpy(maps.k, c.map_k, sizeof(maps.k));
     memcpy(maps.v, c.map_v, sizeof(maps.v));

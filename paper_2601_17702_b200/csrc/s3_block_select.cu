@@ -284,13 +284,8 @@ template <class T, int D, int TT, int THREADS>
 s3_status launch_one(SelectArgs& a, cudaStream_t stream)
 {
     const size_t smem = static_cast<size_t>(MMA_TOKENS) * D + static_cast<size_t>(TT) * a.nb_cap * 4;
-    static bool raised[64] = {};                 // the attribute is kept per device; setting it twice does no harm
-    int dev = 0;
-    S3_CUDA_TRY(cudaGetDevice(&dev));
-    if (dev >= 64 || !raised[dev]) {
-        S3_CUDA_TRY(cudaFuncSetAttribute(select_kernel<T, D, TT, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 << 10));
-        if (dev < 64) raised[dev] = true;
-    }
+    const s3_status allowed = allow_smem<select_kernel<T, D, TT, THREADS>>(200 << 10);
+    if (allowed != S3_OK) return allowed;
     a.one_item_per_seq = a.b.max_q <= TT;
     const int64_t items = a.one_item_per_seq ? a.b.n_seqs : static_cast<int64_t>(a.b.T) / TT + a.b.n_seqs;
     S3_REQUIRE(items * a.n_kv_heads < (int64_t(1) << 31), S3_ERR_UNSUPPORTED, "the batch needs too many thread blocks");

@@ -6,6 +6,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <atomic>
 #include <utility>
 
 #include "s3_common.cuh"
@@ -32,6 +33,21 @@ inline s3_status launch_overlapped(void (*kernel)(Params...), dim3 grid, int thr
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     S3_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, std::forward<Args>(args)...));
+    return S3_OK;
+}
+
+// Lets a kernel use `bytes` of dynamic shared memory; asked once per kernel and device.
+template <auto Kernel>
+inline s3_status allow_smem(int bytes)
+{
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    S3_CUDA_TRY(cudaGetDevice(&dev));
+    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+    if (!(done.load(std::memory_order_relaxed) & bit)) {
+        S3_CUDA_TRY(cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+        done.fetch_or(bit, std::memory_order_relaxed);
+    }
     return S3_OK;
 }
 
