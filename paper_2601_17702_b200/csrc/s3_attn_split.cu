@@ -381,88 +381,80 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                     for (int x = 4; x < 32; x <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], x);
 
             // ---- the four accumulators: 2 -> 0 and 3 -> 1, then 1 -> 0 ----
-            auto at = [&](float* slot, int n, int k, int j) -> float& {
-                return slot[(n * 8 + quad * 2 + (j & 1)) * L::PITCH + k * 16 + (j >> 1) * 8 + r8];
-            };
-            auto put = [&](float* slot, int x, uint64_t* bar) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) at(slot, n, k, j) = o[n][k][j];
-                    if (r8 == 0)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) { red_m[x][n * 8 + quad * 2 + i] = m[n][i]; red_l[x][n * 8 + quad * 2 + i] = l[n][i]; }
-                }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar);
-            };
-            auto take = [&](float* slot, int x) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    float f[2], g[2];
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const float m2 = red_m[x][n * 8 + quad * 2 + i], top = fmaxf(m[n][i], m2), ref = top == -INFINITY ? 0.0f : top;
-                        f[i] = ex2(m[n][i] - ref);
-                        g[i] = ex2(m2 - ref);
-                        m[n][i] = top;
-                        l[n][i] = l[n][i] * f[i] + red_l[x][n * 8 + quad * 2 + i] * g[i];
-                    }
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) o[n][k][j] = o[n][k][j] * f[j & 1] + at(slot, n, k, j) * g[j & 1];
-                }
-                __syncwarp();
-            };
-            const uint32_t now = units & 1, before = (units - 1) & 1;
+            // One copy of the code for both steps: it runs once per unit, and what a short call waits for here is instructions.
             auto wait = [&](uint64_t* bar, uint32_t parity) {
                 ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
                 if (!ok) give_up(DEV_TIMEOUT_ACC_FULL);
                 return ok;
             };
-            if (warp == 2) {
-                if (units > 0 && !wait(&free0, before)) break;
-                put(slot0, 0, &from2);
-            } else if (warp == 3) {
-                if (units > 0 && !wait(&free1, before)) break;
-                put(slot1, 1, &from3);
-            } else if (warp == 1) {
-                if (!wait(&from3, now)) break;
-                take(slot1, 1);
-                put(slot1, 1, &from1);
-            } else {
-                if (!wait(&from2, now)) break;
-                take(slot0, 0);
-                if (!wait(&from1, now)) break;
-                take(slot1, 1);
-                if (lane == 0) mbar_arrive(&free1);
-                float inv[NT][2];
+            const uint32_t now = units & 1;                           // every barrier here completes once per unit
+#pragma unroll 1
+            for (int step = 0; step < 2 && ok; ++step) {
+                const int x = step == 0 ? warp & 1 : 1;               // slot
+                float* slot = x == 0 ? slot0 : slot1;
+                auto at = [&](int n, int k, int j) -> float& {
+                    return slot[(n * 8 + quad * 2 + (j & 1)) * L::PITCH + k * 16 + (j >> 1) * 8 + r8];
+                };
+                if (step == 0 ? warp >= 2 : warp == 1) {
+                    if (step == 0 && units > 0 && !wait(x == 0 ? &free0 : &free1, now ^ 1)) break;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) at(n, k, j) = o[n][k][j];
+                        if (r8 == 0)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) { red_m[x][n * 8 + quad * 2 + i] = m[n][i]; red_l[x][n * 8 + quad * 2 + i] = l[n][i]; }
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(step == 1 ? &from1 : x == 0 ? &from2 : &from3);
+                } else if (step == 0 ? warp < 2 : warp == 0) {
+                    if (!wait(step == 1 ? &from1 : x == 0 ? &from2 : &from3, now)) break;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        float f[2], g[2];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const float m2 = red_m[x][n * 8 + quad * 2 + i], top = fmaxf(m[n][i], m2), ref = top == -INFINITY ? 0.0f : top;
+                            f[i] = ex2(m[n][i] - ref);
+                            g[i] = ex2(m2 - ref);
+                            m[n][i] = top;
+                            l[n][i] = l[n][i] * f[i] + red_l[x][n * 8 + quad * 2 + i] * g[i];
+                        }
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) o[n][k][j] = o[n][k][j] * f[j & 1] + at(n, k, j) * g[j & 1];
+                    }
+                    __syncwarp();
+                    if (step == 1 && lane == 0) mbar_arrive(&free1);
+                }
+            }
+            if (!ok) break;
+            if (warp == 0) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        inv[n][i] = l[n][i] == 0.0f ? 0.0f : 1.0f / l[n][i];
+                        const float inv = l[n][i] == 0.0f ? 0.0f : 1.0f / l[n][i];
                         const int row = n * 8 + quad * 2 + i;
                         if (r8 == 0 && row < info.rows) {
-                            const int64_t out_row = static_cast<int64_t>(info.tok0 + token_of(row)) * a.n_heads + info.head * a.group + head_of(row);
                             const float lse2 = l[n][i] == 0.0f ? -INFINITY : m[n][i] + log2f(l[n][i]);
                             if (info.slot >= 0) a.part_lse[info.slot * a.rows_cap + row] = lse2;
-                            else if (a.lse) a.lse[out_row] = lse2 * kLn2;
+                            else if (a.lse) a.lse[static_cast<int64_t>(info.tok0 + token_of(row)) * a.n_heads + info.head * a.group + head_of(row)] = lse2 * kLn2;
                         }
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j)
+                                slot0[row * L::PITCH + k * 16 + j * 8 + r8] = l[n][i] == 0.0f ? 0.0f : o[n][k][2 * j + i] * inv;
                     }
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) at(slot0, n, k, j) = l[n][j & 1] == 0.0f ? 0.0f : o[n][k][j] * inv[n][j & 1];
                 __syncwarp();
                 // whole rows, 32 / (D / 4) at a time
                 constexpr int LANES = D / 4, STEP = 32 / LANES;
                 const int c = lane % LANES * 4;
+#pragma unroll 1
                 for (int row = lane / LANES; row < info.rows; row += STEP) {
                     const float4 y = *reinterpret_cast<const float4*>(slot0 + row * L::PITCH + c);
                     if (info.slot >= 0) {
