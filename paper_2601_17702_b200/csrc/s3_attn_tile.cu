@@ -224,7 +224,7 @@ __device__ __forceinline__ void transpose_pieces(uint32_t (&v)[8][4], int lane)
     }
 }
 
-template <class T, int D, bool PAIR>
+template <class T, int D, bool PAIR, bool MASKED>
 __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant__ Maps maps, const __grid_constant__ AttnArgs a)
 {
     using L = Layout<D, PAIR>;
@@ -282,8 +282,13 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
     auto tm_o = [&](int i) { return tmem + 256 + 128 * i; };           // its accumulator
     const int tile_tok = min(BM / a.group, a.tok_per_item);            // tokens per 128-row tile
 
+    const bool placed = a.list_mode != LIST_NONE || MASKED;           // the producer says where a tile's keys are
     // First position of virtual key v (a multiple of 16), or -1 where no block is listed.
     auto pos_of = [&](const AttnItem& it, int head, int v) -> int {
+        if (MASKED) {
+            const uint32_t* seen = a.unions + (static_cast<int64_t>(item_number(a, it)) * a.list_heads + (a.list_heads == 1 ? 0 : head)) * a.mask_words;
+            return __ldg(seen + (v >> a.page_shift >> 5)) >> (v >> a.page_shift & 31) & 1u ? v : -1;
+        }
         if (a.list_mode == LIST_NONE) return v;
         const int e = v >> a.page_shift;
         if (e >= a.s || it.pos_last < 0) return -1;
@@ -294,10 +299,10 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
     };
     // Whether key tile `tile` of the block (at v0 of its segment) has rows without a position: their values have to be zeroed.
     auto unclean = [&](const AttnItem& it, int v0, uint32_t tile) -> bool {
-        return a.list_mode == LIST_NONE ? v0 + BN > it.kv : where[tile % 8].unclean != 0;
+        return !placed ? v0 + BN > it.kv : where[tile % 8].unclean != 0;
     };
     // First position of the u-th 16 keys of that tile.
-    auto pos_at = [&](int v0, uint32_t tile, int u) -> int { return a.list_mode == LIST_NONE ? v0 + 16 * u : where[tile % 8].pos[u]; };
+    auto pos_at = [&](int v0, uint32_t tile, int u) -> int { return !placed ? v0 + 16 * u : where[tile % 8].pos[u]; };
     auto give_up = [&](uint32_t code) {
         dev_set_error(a.status, code);
         *abort_flag = 1;
@@ -368,7 +373,7 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
                     if (round > 0 && !wait(&empty_bar[st], (round - 1) & 1)) return false;
                     const bool mine = lane < per_tile && page >= 0;
                     const uint32_t boxes = __popc(__ballot_sync(0xffffffffu, mine));
-                    if (!value && a.list_mode != LIST_NONE) {
+                    if (!value && placed) {
                         TileWhere& w = where[(first_tile + j) % 8];
                         const int units = box / 16;
                         const bool part = lane < per_tile && (page < 0 || pos + box > g.it.kv);
@@ -543,6 +548,12 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
             const int qhi = a.causal ? min(qlo + tile_tok - 1, info.it.pos_last) : qlo;
             float m = -INFINITY, l = 0.0f;                             // reference of the exponentials (scaled, base 2), sum
             int turns = 0;
+            // the row's blocks, where lists came as masks: those of a key tile are in one word (a tile holds 1, 2, 4 or 8)
+            const uint32_t* mask_row = MASKED && live ? a.masks + (static_cast<int64_t>(info.it.tok0 + tok) * a.list_heads +
+                                                                    (a.list_heads == 1 ? 0 : info.head)) * a.mask_words : nullptr;
+            const uint32_t all_bits = (1u << (BN >> a.page_shift)) - 1;
+            uint32_t bits = all_bits;
+            auto bits_of = [&](int v) { return __ldg(mask_row + (v >> a.page_shift >> 5)) >> (v >> a.page_shift & 31) & all_bits; };
             for (int j = PAIR ? 0 : i; j < info.n_tiles; j += PAIR ? 1 : 2, ++turns, ++turn) {
                 ok = __all_sync(0xffffffffu, mbar_wait(&s_full[i], turn & 1, abort_flag));
                 if (!ok) break;
@@ -551,8 +562,9 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
                 const uint32_t tile = tile0 + j;
                 float s[4][32];
                 tm_ld32(my_s, s[0]);
+                if (MASKED) bits = mask_row ? bits_of(v0) : 0u;
                 bool look;                                             // some row may not see some key, or there is no reference yet
-                if (a.list_mode == LIST_NONE) look = v0 + BN - 1 > qlo || (a.window > 0 && v0 <= qhi - a.window);
+                if (!placed) look = v0 + BN - 1 > qlo || (a.window > 0 && v0 <= qhi - a.window);
                 else {
                     look = false;
 #pragma unroll
@@ -561,8 +573,8 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
                         look |= pos < 0 || pos + 15 > qlo || (a.window > 0 && pos <= qhi - a.window);
                     }
                 }
-                const bool edge = look;
-                look |= turns == 0;
+                const bool edge = look, part = MASKED && __any_sync(0xffffffffu, live && bits != all_bits);
+                look |= part || turns == 0;
                 wait_ld();
 #pragma unroll
                 for (int c = 1; c < 4; ++c) tm_ld32(my_s + 32 * c, s[c]);
@@ -579,11 +591,20 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
                         if (edge) {
 #pragma unroll
                             for (int u = 0; u < BN / 16; ++u) {
-                                const int pos = pos_at(v0, tile, u);
+                                int pos = pos_at(v0, tile, u);
+                                if (MASKED && !(bits >> (16 * u >> a.page_shift) & 1u)) pos = -1;
                                 const int hi = pos < 0 ? -1 : qpos - pos, lo = a.window > 0 ? hi - a.window : -1;      // visible: lo < c <= hi
 #pragma unroll
                                 for (int c = 0; c < 16; ++c)
                                     if (c > hi || c <= lo) s[u / 2][u % 2 * 16 + c] = -INFINITY;
+                            }
+                        } else if (part) {
+#pragma unroll
+                            for (int u = 0; u < BN / 16; ++u) {
+                                const bool off = !(bits >> (16 * u >> a.page_shift) & 1u);
+#pragma unroll
+                                for (int c = 0; c < 16; ++c)
+                                    if (off) s[u / 2][u % 2 * 16 + c] = -INFINITY;
                             }
                         }
                         const float a_lo = max_of(s[0]), b_lo = max_of(s[1]), a_hi = max_of(s[2]), b_hi = max_of(s[3]);
@@ -743,11 +764,44 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
     }
 }
 
-template <class T, int D, bool PAIR>
+// Lists per token -> masks, and their union over the tokens of an item: a block per item and list head, a warp per token. Entries
+// past the masks' width are past every sequence's end.
+constexpr int MASK_WARPS = 32;
+__global__ void __launch_bounds__(32 * MASK_WARPS) mask_kernel(const AttnArgs a)
+{
+    __shared__ uint32_t row[MASK_WARPS][kMaxMaskWords], all[kMaxMaskWords];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, words = a.mask_words;
+    for (int w = threadIdx.x; w < words; w += blockDim.x) all[w] = 0u;
+    cudaTriggerProgrammaticLaunchCompletion();
+    cudaGridDependencySynchronize();
+    __syncthreads();
+    AttnItem it;
+    if (!attn_item(a, blockIdx.x, it)) return;                         // the same for every warp
+    for (int tok = warp; tok < it.n_tok; tok += MASK_WARPS) {
+        const int64_t list = static_cast<int64_t>(it.tok0 + tok) * a.list_heads + blockIdx.y;
+        for (int w = lane; w < words; w += 32) row[warp][w] = 0u;
+        __syncwarp();
+        for (int e = lane; e < a.s; e += 32) {
+            const int id = a.lists[list * a.s + e];
+            if (id >= 0 && id < words * 32) atomicOr(&row[warp][id >> 5], 1u << (id & 31));
+        }
+        __syncwarp();
+        for (int w = lane; w < words; w += 32) {
+            a.masks[list * words + w] = row[warp][w];
+            if (row[warp][w]) atomicOr(&all[w], row[warp][w]);
+        }
+        __syncwarp();
+    }
+    __syncthreads();
+    uint32_t* out = a.unions + (static_cast<int64_t>(item_number(a, it)) * a.list_heads + blockIdx.y) * words;
+    for (int w = threadIdx.x; w < words; w += blockDim.x) out[w] = all[w];
+}
+
+template <class T, int D, bool PAIR, bool MASKED>
 s3_status launch_tile(const KvCacheState& c, const AttnArgs& a, cudaStream_t stream)
 {
     using L = Layout<D, PAIR>;
-    const s3_status allowed = allow_smem<tile_kernel<T, D, PAIR>>(L::TOTAL);
+    const s3_status allowed = allow_smem<tile_kernel<T, D, PAIR, MASKED>>(L::TOTAL);
     if (allowed != S3_OK) return allowed;
     Maps maps;
     memcpy(maps.k, c.map_k, sizeof(maps.k));
@@ -755,16 +809,23 @@ s3_status launch_tile(const KvCacheState& c, const AttnArgs& a, cudaStream_t str
     const int tile_tok = BM / a.group < a.tok_per_item ? BM / a.group : a.tok_per_item;
     s3_status st = make_kv_query_map(maps.q, c, a.q, a.ldq, a.b.T, a.group, tile_tok);
     if (st != S3_OK) return st;
-    return launch_overlapped(tile_kernel<T, D, PAIR>, dim3(a.grid), THREADS, L::TOTAL, stream, maps, a);
+    return launch_overlapped(tile_kernel<T, D, PAIR, MASKED>, dim3(a.grid), THREADS, L::TOTAL, stream, maps, a);
 }
 
 template <class T, int D>
 s3_status launch_dim(const KvCacheState& c, const AttnArgs& a, cudaStream_t stream)
 {
-    return a.tok_per_item > BM / a.group ? launch_tile<T, D, true>(c, a, stream) : launch_tile<T, D, false>(c, a, stream);
+    // masks as a variant of their own: in one kernel with the others they cost those 4 % (registers), lists or not
+    if (a.tok_per_item > BM / a.group) return a.masks ? launch_tile<T, D, true, true>(c, a, stream) : launch_tile<T, D, true, false>(c, a, stream);
+    return a.masks ? launch_tile<T, D, false, true>(c, a, stream) : launch_tile<T, D, false, false>(c, a, stream);
 }
 
 }  // namespace
+
+s3_status launch_attn_masks(const AttnArgs& a, cudaStream_t stream)
+{
+    return launch_overlapped(mask_kernel, dim3(a.n_items, a.list_heads), 32 * MASK_WARPS, 0, stream, a);
+}
 
 s3_status launch_attn_tile(const KvCacheState& c, const AttnArgs& a, cudaStream_t stream)
 {

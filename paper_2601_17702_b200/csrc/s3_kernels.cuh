@@ -115,6 +115,7 @@ s3_status launch_block_select(const KvCacheState& c, const KvBatchDev& b, const 
                               int n_first, int n_last, int32_t* d_blocks, uint32_t* d_status, cudaStream_t stream);
 s3_status launch_attn_split(const KvCacheState& c, const AttnArgs& a, cudaStream_t stream);   // at most 16 query rows per item
 s3_status launch_attn_tile(const KvCacheState& c, const AttnArgs& a, cudaStream_t stream);    // tiles of 128 query rows
+s3_status launch_attn_masks(const AttnArgs& a, cudaStream_t stream);
 s3_status launch_attn_join(const KvCacheState& c, const AttnArgs& a, bool tile, cudaStream_t stream);    // joins the pieces of either
 
 }  // namespace s3

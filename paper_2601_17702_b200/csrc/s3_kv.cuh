@@ -122,6 +122,8 @@ __device__ __forceinline__ int seq_of_row(const KvBatchDev& b, int t)
     return lo;
 }
 
+constexpr int kMaxMaskWords = 128;      // 4096 blocks
+
 enum { LIST_NONE = 0, LIST_PER_TOKEN = 1, LIST_PER_SEQ = 2 };
 
 // Launch parameters of the attention kernels.
@@ -131,10 +133,14 @@ enum { LIST_NONE = 0, LIST_PER_TOKEN = 1, LIST_PER_SEQ = 2 };
 // position block(v / page_size) * page_size + v % page_size, block(e) = e for the whole cache and = list[e] for a list, and
 // are taken in tiles from the first one that some row of the item sees.
 //
+// Lists per token have a second form, for chunks whose lists cover a good part of a short context: the keys are counted as for the
+// whole cache, a bit per token and block says who may see it (masks), and blocks that no token of an item lists (unions) count as
+// not there: they are neither looked up nor read. A key tile then serves an item's rows instead of a token's.
+//
 // The grid's thread blocks share the work in one of two ways, which the host chooses:
 //   share = 0   unit u = (key head, item), whole, goes to block u mod grid; key head by key head, so that the blocks are at work on
 //               the keys of one head or two, which the L2 cache holds when a token's list picks among many (1024 tokens x 16 of
-//               512 blocks: 360 -> 240 us);
+//               512 blocks: 359 -> 333 us);
 //   share > 0   the tiles of all units, laid end to end (key head by key head, item by item), are cut into equal shares of `share`
 //               tiles or less, one per block, whatever the lengths are. A unit that a cut divides is worked on in pieces; a
 //               piece's result goes to a slot of its block (each has at most two pieces: one that began before its share and
@@ -146,6 +152,9 @@ struct AttnArgs {
     int32_t causal, window;
     const int32_t* lists;
     int32_t s, list_heads, list_mode;
+    uint32_t* masks;            // [T][list_heads][mask_words] or null
+    uint32_t* unions;           // [item_number()][list_heads][mask_words]
+    int32_t mask_words;
     const void* q;
     int64_t ldq;
     void* out;
@@ -176,6 +185,9 @@ __device__ __forceinline__ AttnItem make_item(const AttnArgs& a, int seq, const 
     it.list = a.list_mode == LIST_PER_TOKEN ? it.tok0 : seq;
     return it;
 }
+
+// A number of its own for every item: first rows rise by tok_per_item within a sequence, and do not fall from one to the next.
+__device__ __forceinline__ int item_number(const AttnArgs& a, const AttnItem& it) { return it.tok0 / a.tok_per_item + it.seq; }
 
 // First position that some row of the item may see.
 __device__ __forceinline__ int first_seen(const AttnArgs& a, const AttnItem& it)

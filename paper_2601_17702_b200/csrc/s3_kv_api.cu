@@ -57,8 +57,12 @@ constexpr int kSplitRows = 16;             // rows per item up to which the spli
 constexpr int kTileRows = 128;
 
 // How an attention call is cut. None of it depends on the device-side lengths.
+// Modelled time of a pair tile under masks, and of the masks themselves and the start (us).
+constexpr double kMaskedTile = 2.7, kMaskedFixed = 12.0;
+
 struct AttnPlan {
     bool tile;                             // tile kernel, else split kernel
+    bool masked;                           // lists per token as masks over all blocks
     int tok_per_item, n_items, one_item_per_seq;
     int grid, share_min, whole_rounds, rows_cap;
 };
@@ -89,33 +93,70 @@ double choose_shares(AttnPlan& p, const s3_kv_batch& b, int n_kv_heads, int list
     return share;
 }
 
-// keys: the most virtual keys an item can have.
-AttnPlan plan_attention(const s3_kv_batch& b, int group, int n_kv_heads, int list_mode, int64_t keys)
+// Items of several tokens of a sequence; keys: the most virtual keys an item can have; time: modelled, in key tiles.
+AttnPlan plan_tokens(const s3_kv_batch& b, int group, int n_kv_heads, int list_mode, int64_t keys, double& time)
 {
     AttnPlan p;
+    p.masked = false;
+    p.tile = static_cast<int64_t>(b.max_q) * group > kSplitRows;
+    const int one = (p.tile ? kTileRows : kSplitRows) / group;
+    auto items = [&](AttnPlan& q, int tokens) {
+        q.tok_per_item = tokens;
+        q.one_item_per_seq = b.max_q <= tokens;
+        q.n_items = q.one_item_per_seq ? b.n_seqs : b.n_seqs == 1 ? (b.T + tokens - 1) / tokens : b.T / tokens + b.n_seqs;
+    };
+    items(p, one);
+    // With one query tile per item the two softmax groups share the keys: a key tile takes a little more than half the time that it
+    // takes with two, there are twice as many units, and every key is copied twice as often.
+    time = choose_shares(p, b, n_kv_heads, list_mode, keys, p.tile ? 0.6 : 1.0, p.tile ? 6.0 : 12.0);
+    if (p.tile && b.max_q > one) {
+        AttnPlan q = p;
+        items(q, 2 * one);
+        const double pair = choose_shares(q, b, n_kv_heads, list_mode, keys, 1.0, 6.0);
+        if (pair <= time) {
+            p = q;
+            time = pair;
+        }
+    }
+    return p;
+}
+
+int mask_words(const s3_kv_batch& b, int page_shift) { return b.max_kv > 0 ? ((b.max_kv - 1) >> page_shift) / 32 + 1 : 1; }
+
+// Masks of the tokens, and the unions of items of tok_per_item tokens or more.
+size_t mask_bytes(const s3_kv_batch& b, int page_shift, int list_heads, int tok_per_item)
+{
+    const size_t words = mask_words(b, page_shift) < kMaxMaskWords ? mask_words(b, page_shift) : kMaxMaskWords;
+    return round_up(static_cast<size_t>(b.T) * list_heads * words * 4, 256) +
+           round_up((static_cast<size_t>(b.T) / tok_per_item + b.n_seqs) * list_heads * words * 4, 256);
+}
+
+// keys: the most virtual keys an item can have.
+AttnPlan plan_attention(const s3_kv_batch& b, int group, int n_kv_heads, int list_mode, int64_t keys, int page_shift)
+{
+    AttnPlan p;
+    p.masked = false;
     if (list_mode == LIST_PER_TOKEN) {
         p.tile = group > kSplitRows;
         p.tok_per_item = 1;
         p.n_items = b.T;
         p.one_item_per_seq = 0;
-        choose_shares(p, b, n_kv_heads, list_mode, keys, 1.0, p.tile ? 6.0 : 12.0);
-    } else {
-        p.tile = static_cast<int64_t>(b.max_q) * group > kSplitRows;
-        const int one = (p.tile ? kTileRows : kSplitRows) / group;
-        auto items = [&](AttnPlan& q, int tokens) {
-            q.tok_per_item = tokens;
-            q.one_item_per_seq = b.max_q <= tokens;
-            q.n_items = q.one_item_per_seq ? b.n_seqs : b.n_seqs == 1 ? (b.T + tokens - 1) / tokens : b.T / tokens + b.n_seqs;
-        };
-        items(p, one);
-        // With one query tile per item the two softmax groups share the keys: a key tile takes a little more than half the time that it
-        // takes with two, there are twice as many units, and every key is copied twice as often.
-        const double single = choose_shares(p, b, n_kv_heads, list_mode, keys, p.tile ? 0.6 : 1.0, p.tile ? 6.0 : 12.0);
-        if (p.tile && b.max_q > one) {
-            AttnPlan q = p;
-            items(q, 2 * one);
-            if (choose_shares(q, b, n_kv_heads, list_mode, keys, 1.0, 6.0) <= single) p = q;
+        const double listed = choose_shares(p, b, n_kv_heads, list_mode, keys, 1.0, p.tile ? 6.0 : 12.0) * (p.tile ? 2.0 : 0.7);     // us
+        // As masks over the blocks that an item lists: a key tile's copies and products serve up to 256 rows, in vain where a row
+        // does not list the block, so it pays where the lists are a good part of the context. Measured as lists and as masks, 1024
+        // tokens of 4 x 8 heads, 16 random blocks of 64 of each: over 2K keys 325 and 57 us, 8K 325 and 175, 16K 326 and 331, 32K 326
+        // and 845; 32 tokens over 2K keys 16.5 and 24.8. The two constants are fitted to these.
+        if (static_cast<int64_t>(b.max_q) * group > kSplitRows && mask_words(b, page_shift) <= kMaxMaskWords) {
+            double over_all;
+            AttnPlan q = plan_tokens(b, group, n_kv_heads, LIST_NONE, b.max_kv, over_all);
+            if (over_all * kMaskedTile + kMaskedFixed < listed) {
+                p = q;
+                p.masked = true;
+            }
         }
+    } else {
+        double time;
+        p = plan_tokens(b, group, n_kv_heads, list_mode, keys, time);
     }
     p.rows_cap = p.tile ? p.tok_per_item * group : kSplitRows;
     return p;
@@ -126,7 +167,7 @@ size_t partial_bytes(const AttnPlan& p, int head_dim)
 {
     if (p.share_min == 0) return 0;
     const size_t rows = 2 * static_cast<size_t>(p.grid) * p.rows_cap;
-    return round_up(rows * head_dim * 4, 256) + round_up(rows * 4, 256) + static_cast<size_t>(p.grid) * sizeof(Cut);
+    return round_up(rows * head_dim * 4, 256) + round_up(rows * 4, 256) + round_up(static_cast<size_t>(p.grid) * sizeof(Cut), 256);
 }
 
 }  // namespace
@@ -209,7 +250,8 @@ s3_status attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const vo
     S3_TRY(check_rows("d_out", d_out, ld_out, n_heads, c.d.head_dim));
     S3_REQUIRE(d_ws != nullptr && ws_bytes >= S3_WS_HEADER_BYTES, S3_ERR_CAPACITY, "workspace missing or smaller than %d bytes", S3_WS_HEADER_BYTES);
     const int group = n_heads / c.d.n_kv_heads;
-    const AttnPlan p = plan_attention(b, group, c.d.n_kv_heads, list_mode, list_mode == LIST_NONE ? b.max_kv : static_cast<int64_t>(s) << c.page_shift);
+    const AttnPlan p = plan_attention(b, group, c.d.n_kv_heads, list_mode, list_mode == LIST_NONE ? b.max_kv : static_cast<int64_t>(s) << c.page_shift,
+                                      c.page_shift);
 
     AttnArgs a;
     memset(&a, 0, sizeof(a));
@@ -243,8 +285,8 @@ s3_status attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const vo
     a.share_min = p.share_min;
     a.whole_rounds = p.whole_rounds;
     a.rows_cap = p.rows_cap;
-    const size_t need = 256 + partial_bytes(p, c.d.head_dim);
-    S3_REQUIRE(p.share_min == 0 || ws_bytes >= need, S3_ERR_CAPACITY, "workspace holds %zu bytes, %zu needed", ws_bytes, need);
+    const size_t partial = partial_bytes(p, c.d.head_dim), need = 256 + partial + (p.masked ? mask_bytes(b, c.page_shift, list_heads, p.tok_per_item) : 0);
+    S3_REQUIRE((p.share_min == 0 && !p.masked) || ws_bytes >= need, S3_ERR_CAPACITY, "workspace holds %zu bytes, %zu needed", ws_bytes, need);
     if (p.share_min > 0) {
         const size_t rows = 2 * static_cast<size_t>(p.grid) * p.rows_cap;
         a.part_o = reinterpret_cast<float*>(static_cast<unsigned char*>(d_ws) + 256);
@@ -252,6 +294,14 @@ s3_status attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const vo
         a.cuts = reinterpret_cast<int32_t*>(reinterpret_cast<unsigned char*>(a.part_lse) + round_up(rows * 4, 256));
     }
     const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (p.masked) {
+        unsigned char* at = static_cast<unsigned char*>(d_ws) + 256 + partial;
+        a.mask_words = mask_words(b, c.page_shift);
+        a.masks = reinterpret_cast<uint32_t*>(at);
+        a.unions = reinterpret_cast<uint32_t*>(at + round_up(static_cast<size_t>(b.T) * list_heads * a.mask_words * 4, 256));
+        a.list_mode = LIST_NONE;
+        S3_TRY(launch_attn_masks(a, st));
+    }
     S3_TRY(p.tile ? launch_attn_tile(c, a, st) : launch_attn_split(c, a, st));
     return p.share_min > 0 && p.grid > 1 ? launch_attn_join(c, a, p.tile, st) : S3_OK;
 }
@@ -330,7 +380,7 @@ size_t s3_kv_workspace_bytes(const s3_kv_cache* cache, const s3_kv_batch* batch,
             const size_t bytes = partial_bytes(p, cache->st.d.head_dim);
             if (bytes > most) most = bytes;
         }
-    return 256 + most;
+    return 256 + most + (batch->T > 0 && batch->n_seqs > 0 ? mask_bytes(*batch, cache->st.page_shift, cache->st.d.n_kv_heads, kTileRows * cache->st.d.n_kv_heads / n_heads) : 0);
 }
 
 s3_status s3_kv_append(const s3_kv_cache* cache, const s3_kv_batch* batch, const s3_rope* rope, const int32_t* d_positions,

@@ -571,3 +571,41 @@ def test_example_runs_them_together():
     question, answer, found = m.run(context=4096, chunk=1024)
     # the stretch asked about is one page of 64, and holds nearly all of the attention's weight
     assert found and question > 0.9 and min(answer) > 0.9
+
+
+@pytest.mark.parametrize("lens", [[(300, 900)], [(130, 640), (0, 70), (260, 260), (1, 333), (90, 41)]])
+@pytest.mark.parametrize("H,K,D,P,n,dtype,causal,window", [(8, 8, 128, 64, 9, torch.bfloat16, True, 0), (8, 2, 64, 16, 40, torch.float16, True, 0),
+                                                           (8, 8, 128, 128, 6, torch.float16, True, 200), (14, 2, 128, 32, 12, torch.bfloat16, False, 0),
+                                                           (6, 2, 128, 16, 24, torch.bfloat16, False, 150)])
+def test_listed_blocks_that_cover_much_of_a_chunks_context(lens, H, K, D, P, n, dtype, causal, window):
+    """Many rows whose lists are a good part of a short context. Blocks that no row lists hold NaN, their table entries no page."""
+    s = R.Setup(lens, H, K, D, P, dtype, seed=P + n)
+    for heads in {1, K}:
+        lists = some_lists(s, n, heads, True, seed=n)
+        skipped = lambda i, j: (7 * i + j) % 3 == 1
+        for row, i, _ in s.rows():
+            for b in range(s.cols + 1):
+                if skipped(i, b):
+                    lists[row][lists[row] == b] = -1
+        t = R.Setup(lens, H, K, D, P, dtype, seed=P + n)
+        for i, (_, kv) in enumerate(lens):
+            for j in range(-(-kv // P)):
+                if skipped(i, j):
+                    page = int(t.pages[i, j])
+                    t.k_cache[page], t.v_cache[page] = float("nan"), float("nan")
+                    if j % 2:
+                        t.pages[i, j] = 2**31 - 1 if j % 4 == 1 else -5
+        d = Device(t)
+        out, lse = S.s3_block_attention(d.cache, d.batch, d.q, dev(lists), d.ws, causal=causal, window=window, want_lse=True)
+        d.fine()
+        check(s, out, lse, *R.attention(s, causal=causal, window=window, blocks=lists))
+
+
+def test_listed_blocks_of_a_chunk_whose_cached_positions_are_none():
+    s = R.Setup([(200, 0)], 8, 8, 128, 16, seed=2)
+    d = Device(s)
+    lists = torch.zeros((s.T, 8, 20), dtype=torch.int32, device="cuda")
+    lists += torch.arange(20, dtype=torch.int32, device="cuda")
+    out, lse = S.s3_block_attention(d.cache, d.batch, d.q, lists, d.ws, want_lse=True)
+    d.fine()
+    assert (out == 0).all() and (lse == -math.inf).all()
