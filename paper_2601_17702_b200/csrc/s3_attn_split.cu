@@ -10,8 +10,8 @@
 // Warps 0-3 take 16 keys of every tile each and keep their own reference, sum and accumulator in registers, so the warps meet
 // only at the end of a unit. Both products are taken transposed, S^T = K Q^T and O^T = V^T P^T (mma.sync m16n8k16): the 16-wide
 // side of the instruction holds keys and dimensions, the 8-wide side the query rows, of which a group of 4 or 7 fills most.
-// P^T changes its fragment form in registers (movmatrix). The reference moves only when a score exceeds it by 2^8, which one
-// warp vote decides; weights then stay below 2^8, inside either type. With this few rows per key the work is a copy.
+// P^T changes its fragment form in registers (movmatrix). The reference moves only when a score exceeds it by 2^8 (f16: 2^15, see
+// WeightRange), which one warp vote decides; weights stay inside either type. With this few rows per key the work is a copy.
 // Measured on a B200 whose copies run at 6.53 TB/s: one token of 4 x 8 heads over 131072 keys 92 us (5.9 TB/s); 64 tokens over up to
 // 8192 keys 94 us; 1024 tokens over 16 of 512 blocks each 327 us, where the 4.3 GB through the SMs' read ports bound (245 us at 64 bytes
 // per clock and SM), 93 % of them hits in L2.
@@ -30,7 +30,6 @@ using namespace kv;
 constexpr int TILE = 64;                  // keys per tile
 constexpr int WARPS = 4;                  // compute warps
 constexpr int THREADS = 32 * (WARPS + 1);
-constexpr float RESCALE_AT = 8.0f;
 
 struct Maps {
     alignas(64) unsigned char k[128], v[128];
@@ -92,6 +91,7 @@ template <class T, int D, int NT>
 __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant__ Maps maps, const __grid_constant__ AttnArgs a)
 {
     using L = Layout<D, NT>;
+    using Range = WeightRange<T>;
     constexpr int STAGES = L::STAGES;
     extern __shared__ __align__(1024) unsigned char ring[];           // swizzled tiles start on 1024-byte boundaries
     __shared__ uint64_t full_bar[STAGES], empty_bar[STAGES], unit_full[2], unit_empty[2];
@@ -324,7 +324,7 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                             const int i = j & 1, kp = pos + r8 + (j >> 1) * 8;
                             sc[n][j] *= a.scale_log2;
                             if (edge && (kp > qpos[n][i] || (a.window > 0 && kp <= qpos[n][i] - a.window))) sc[n][j] = -INFINITY;
-                            grow |= sc[n][j] > m[n][i] + RESCALE_AT;
+                            grow |= sc[n][j] > m[n][i] + Range::grow;
                         }
                     if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                             float f[2];
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {
-                                float top = fmaxf(fmaxf(sc[n][i], sc[n][2 + i]), m[n][i]);
+                                float top = fmaxf(fmaxf(sc[n][i], sc[n][2 + i]) - Range::lift, m[n][i]);
                                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));

@@ -15,7 +15,7 @@
 // and the odd key tiles, with an accumulator each, and are joined at the end. Either way one group's exponentials run while
 // the tensor core works for the other: the two sides need about the same time at head_dim 128.
 // O stays in tensor memory. It is rescaled only when a row's maximum has grown far over the reference its exponentials use (P
-// stays below 2^14, inside either type, and the sum in fp32); the MMA order makes S(j+1) complete
+// stays inside the type, see WeightRange, and the sum in fp32); the MMA order makes S(j+1) complete
 // only after O += P(j) V(j), so the group may touch O as soon as it sees the next S.
 //
 // Measured: 2048 tokens of 4 x 8 heads at the end of 32768 keys in 909 to 963 us (1.11 to 1.17 PFLOP/s; 1.63 is what a large library
@@ -37,8 +37,6 @@ using namespace kv;
 constexpr int BM = 128, BN = 128;                  // query rows and keys per tile
 constexpr int THREADS = 384;
 constexpr int TMEM_COLS = 512;
-constexpr float RESCALE_AT = 8.0f;                 // a reference is moved to the row's maximum when that exceeds it by this,
-constexpr float CHECK_AT = 14.0f;                  // which is looked at when a weight may exceed 2^14
 
 struct Maps {
     alignas(64) unsigned char q[128], k[128], v[128];
@@ -232,6 +230,7 @@ template <class T, int D, bool PAIR, bool MASKED>
 __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant__ Maps maps, const __grid_constant__ AttnArgs a)
 {
     using L = Layout<D, PAIR>;
+    using Range = WeightRange<T>;
     constexpr int SLOTS = L::SLOTS, AHEAD = PAIR ? 1 : 2;       // key tiles whose S is issued before the first P V
     extern __shared__ __align__(1024) unsigned char smem[];            // swizzled tiles start on 1024-byte boundaries
     unsigned char* ring = smem + L::RING;
@@ -539,6 +538,7 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
         const int first_tok = PAIR ? i * tile_tok : 0;                 // first token of the tile, relative to the item
         const int tok = first_tok + row / a.group, g = row % a.group;
         const f32x2 scale2 = pair_of(a.scale_log2, a.scale_log2);
+        constexpr float most = static_cast<float>(1 << static_cast<int>(Range::most));
         uint32_t turn = 0, tile0 = 0;                                  // key tiles this group has taken; the block's before this segment
         bool ok = true;
         for (int seg = 0;; ++seg) {
@@ -613,9 +613,9 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
                         }
                         const float a_lo = max_of(s[0]), b_lo = max_of(s[1]), a_hi = max_of(s[2]), b_hi = max_of(s[3]);
                         const float top = fmaxf(fmaxf(a_lo, b_lo), fmaxf(a_hi, b_hi)) * a.scale_log2;
-                        const bool grow = live && top > m + RESCALE_AT;
+                        const bool grow = live && top > m + Range::grow;
                         if (__any_sync(0xffffffffu, grow)) {
-                            const float now = grow ? top : m;
+                            const float now = grow ? top - Range::lift : m;
                             const float f = m == -INFINITY ? 0.0f : ex2(m - now);
                             m = now;
                             l *= f;
@@ -640,7 +640,7 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
                     weights<T>(s[1], scale2, ref2, p_lo + 16, sum);
                     if (look) break;
                     const float a_hi = max_of(s[2]), b_hi = max_of(s[3]), top = max3(a_hi, b_hi, b_hi) * a.scale_log2;
-                    look = __any_sync(0xffffffffu, live && !(total(sum) <= 16384.0f && top <= m + CHECK_AT));
+                    look = __any_sync(0xffffffffu, live && !(total(sum) <= most && top <= m + Range::most));
                     if (!look) break;
                 }
                 tm_st32(my_s, p_lo);

@@ -1,0 +1,43 @@
+"""Paged key / value cache operators at the edges: narrow weights, wide windows, pages that a window has left behind, steps that
+follow each other without a pause, misaligned arrays, every variant the host's plan can pick.
+
+Tolerances are those of the tests beside it: eps = 2^-8 (bf16) or 2^-11 (f16); a result is a mean of values under weights rounded
+to the type, each off by at most eps of itself, and is rounded once: |out - exact| <= eps (|out| + mean |v|) + 1e-4, the mean of |v|
+under the exact weights. (f16 weights are lifted so that only those 2^-21 and more below the largest are subnormal; what
+these lose is under 2^-32 each, 2^-15 of the largest weight for the 131072 keys here.)"""
+import math
+
+import pytest
+import torch
+
+import kv_reference as R
+import paper_2601_17702_b200 as S
+from test_gpu_kv import Device, check, dev
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("n,seqs", [(1, 600), (40, 300)])
+@pytest.mark.parametrize("octaves", [18.5, 20.25, 23.5])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_many_keys_far_below_the_largest_weight(n, seqs, octaves, dtype):
+    """A strong first key and 131071 equal ones of weight 2^-octaves each, which together weigh 2^(17 - octaves). As many sequences,
+    all over the same pages, as thread blocks run at a time or more: most of them are not cut into pieces."""
+    s = R.Setup([(n, 131072)], 2, 1, 64, 128, dtype, seed=1, outside=0.0)
+    s.scale = 1.0
+    s.q.zero_()
+    s.q[:, :, 0] = 8.0
+    s.k_cache.zero_()
+    s.v_cache.copy_((1 + torch.arange(64) / 64).to(dtype).expand_as(s.v_cache))
+    first = int(s.pages[0, 0])
+    s.k_cache[first, 0, 0, 0] = octaves * math.log(2.0) / 8
+    s.v_cache[first, 0, 0] = 0
+    want, want_lse = R.attention(s)
+    cache = S.KvCache(dev(s.k_cache), dev(s.v_cache))
+    batch = S.KvBatch(torch.arange(seqs + 1, dtype=torch.int32, device="cuda") * n, torch.full((seqs,), 131072, dtype=torch.int32, device="cuda"),
+                      dev(s.pages.repeat(seqs, 1)), seqs * n, n, 131072)
+    ws = S.new_workspace(S.s3_kv_workspace_bytes(cache, batch, 2))
+    out, lse = S.s3_paged_attention(cache, batch, dev(s.q.repeat(seqs, 1, 1)), ws, scale=1.0, want_lse=True)
+    assert S.s3_workspace_status(ws) == 0
+    want, want_lse = want.repeat(seqs, 1, 1), want_lse.repeat(seqs, 1)
+    check(s, out, lse, want, want_lse, mean_abs=want.abs())
