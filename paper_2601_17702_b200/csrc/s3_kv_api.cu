@@ -266,7 +266,7 @@ s3_status attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const vo
     a.head_dim = c.d.head_dim;
     a.scale_log2 = params->scale * kLog2e;
     a.causal = params->causal != 0;
-    a.window = params->window;
+    a.window = params->window < b.max_kv ? params->window : 0;         // a window that holds every position hides none
     a.lists = d_blocks;
     a.s = s;
     a.list_heads = list_heads;

@@ -41,3 +41,14 @@ def test_many_keys_far_below_the_largest_weight(n, seqs, octaves, dtype):
     assert S.s3_workspace_status(ws) == 0
     want, want_lse = want.repeat(seqs, 1, 1), want_lse.repeat(seqs, 1)
     check(s, out, lse, want, want_lse, mean_abs=want.abs())
+
+
+@pytest.mark.parametrize("lens", [[(4, 2), (1, 30), (3, 0)], [(90, 40), (70, 70), (130, 125)]])
+@pytest.mark.parametrize("window", [2**31 - 1, 2**31 - 30, 41])
+def test_windows_up_to_the_largest_number(lens, window):
+    """More new rows than positions: the first rows' positions are negative, and position - window passes 32 bits."""
+    s = R.Setup(lens, 8, 2, 128, 16, seed=window % 97)
+    d = Device(s)
+    out, lse = S.s3_paged_attention(d.cache, d.batch, d.q, d.ws, window=window, want_lse=True)
+    d.fine()
+    check(s, out, lse, *R.attention(s, window=window))
