@@ -290,12 +290,12 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
     auto pos_of = [&](const AttnItem& it, int head, int v) -> int {
         if (MASKED) {
             const uint32_t* seen = a.unions + (static_cast<int64_t>(item_number(a, it)) * a.list_heads + (a.list_heads == 1 ? 0 : head)) * a.mask_words;
-            return __ldg(seen + (v >> a.page_shift >> 5)) >> (v >> a.page_shift & 31) & 1u ? v : -1;
+            return seen[v >> a.page_shift >> 5] >> (v >> a.page_shift & 31) & 1u ? v : -1;
         }
         if (a.list_mode == LIST_NONE) return v;
         const int e = v >> a.page_shift;
         if (e >= a.s || it.pos_last < 0) return -1;
-        const int id = __ldg(a.lists + (static_cast<int64_t>(it.list) * a.list_heads + (a.list_heads == 1 ? 0 : head)) * a.s + e);
+        const int id = a.lists[(static_cast<int64_t>(it.list) * a.list_heads + (a.list_heads == 1 ? 0 : head)) * a.s + e];
         // a block all of whose positions are out of sight counts as not listed
         if (id < 0 || id > (it.pos_last >> a.page_shift) || ((id + 1) << a.page_shift) <= first_seen(a, it)) return -1;
         return (id << a.page_shift) + (v & (a.page_size - 1));
@@ -352,7 +352,7 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
                     page = -1;
                     pos = t + lane / per_tile < n_tiles ? pos_of(g.it, g.head, v_lo + t * BN + lane * box) : -1;
                     if (pos < 0 || pos >= g.it.kv) return;
-                    const int p = __ldg(table + (pos >> a.page_shift));
+                    const int p = table[pos >> a.page_shift];
                     page = p < 0 || p >= a.n_pages ? a.n_pages : p;    // beyond the map: reads as zeros
                     if (page == a.n_pages) dev_set_error(a.status, DEV_BAD_PAGE);
                 };
@@ -557,7 +557,7 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
                                                                     (a.list_heads == 1 ? 0 : info.head)) * a.mask_words : nullptr;
             const uint32_t all_bits = (1u << (BN >> a.page_shift)) - 1;
             uint32_t bits = all_bits;
-            auto bits_of = [&](int v) { return __ldg(mask_row + (v >> a.page_shift >> 5)) >> (v >> a.page_shift & 31) & all_bits; };
+            auto bits_of = [&](int v) { return mask_row[v >> a.page_shift >> 5] >> (v >> a.page_shift & 31) & all_bits; };
             for (int j = PAIR ? 0 : i; j < info.n_tiles; j += PAIR ? 1 : 2, ++turns, ++turn) {
                 ok = __all_sync(0xffffffffu, mbar_wait(&s_full[i], turn & 1, abort_flag));
                 if (!ok) break;

@@ -228,15 +228,15 @@ __global__ void __launch_bounds__(THREADS, TT == 16 ? 5 : 2) select_kernel(const
 #pragma unroll
         for (int x = 0; x < Q; ++x) c[x] = make_uint4(0, 0, 0, 0);
         if (j >= nb) return;
-        const int page = __ldg(table + j);
+        const int page = table[j];
         if (static_cast<uint32_t>(page) >= static_cast<uint32_t>(a.n_pages)) {
             dev_set_error(a.status, DEV_BAD_PAGE);
             return;
         }
         const int8_t* src = my_code + static_cast<int64_t>(page) * page_pitch;
 #pragma unroll
-        for (int x = 0; x < Q; ++x) c[x] = __ldg(reinterpret_cast<const uint4*>(src + x * 64));
-        scale = __ldg(my_scale + static_cast<int64_t>(page) * a.n_kv_heads);
+        for (int x = 0; x < Q; ++x) c[x] = *reinterpret_cast<const uint4*>(src + x * 64);
+        scale = my_scale[static_cast<int64_t>(page) * a.n_kv_heads];
     };
     auto mma = [](int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
         asm volatile("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"

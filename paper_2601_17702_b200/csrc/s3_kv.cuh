@@ -18,7 +18,9 @@ constexpr float kSumSteps = 4096.0f, kSumLimit = 2047.0f;   // fixed point of th
 
 // Launch that may begin while the kernel before it in the stream ends (programmatic launch): its blocks set themselves up, and
 // cudaGridDependencySynchronize() in the kernel waits for that kernel's end before anything it may have written is read, or
-// anything it may still read is written. Worth about a microsecond per call where calls are short.
+// anything it may still read is written. Worth about a microsecond per call where calls are short. What an earlier kernel may have
+// written is read with ordinary loads: __ldg (ld.global.nc) asks for memory that nobody writes while the kernel lives, and these
+// kernels live while the one before them still writes. Only the rotation tables are read that way.
 template <class... Params, class... Args>
 inline s3_status launch_overlapped(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t stream, Args&&... args)
 {

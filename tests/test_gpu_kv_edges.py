@@ -52,3 +52,68 @@ def test_windows_up_to_the_largest_number(lens, window):
     out, lse = S.s3_paged_attention(d.cache, d.batch, d.q, d.ws, window=window, want_lse=True)
     d.fine()
     check(s, out, lse, *R.attention(s, window=window))
+
+
+def test_steps_that_follow_each_other_without_a_pause():
+    """Launches overlap the one before them: append, select and attend on one cache, one list buffer and one workspace, step after step
+    without waiting for the GPU, give what they give with a pause after every call."""
+    H, K, D, P, n, steps = 8, 2, 128, 16, 3, 40
+    g = torch.Generator().manual_seed(11)
+    start = [400, 90, 250]
+    q, k, v = (torch.randn((steps, n, x, D), generator=g).bfloat16().cuda() for x in (H, K, K))
+    k[:, :, :, :40] *= 3.0
+    held = torch.randn((120, K, P, D), generator=g).bfloat16().cuda()
+    pages = torch.randperm(120, generator=g).to(torch.int32)[:n * 33].view(n, 33).cuda()
+    cu = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    lens = [torch.tensor([x + i + 1 for x in start], dtype=torch.int32, device="cuda") for i in range(steps)]
+
+    def run(pause):
+        cache = S.KvCache.zeros(120, K, P, D)
+        cache.k.copy_(held)
+        cache.v.copy_(held.flip(0))
+        batch = [S.KvBatch(cu, lens[i], pages, n, 1, 33 * P) for i in range(steps)]
+        ws = S.new_workspace(S.s3_kv_workspace_bytes(cache, batch[0], H))
+        first = S.KvBatch(torch.tensor([0, 400, 490, 740], dtype=torch.int32, device="cuda"), torch.tensor(start, dtype=torch.int32, device="cuda"),
+                          pages, 740, 400, 33 * P)
+        prompt = torch.cat([held.flip(1).reshape(-1, K, D)[:740], held.flip(2).reshape(-1, K, D)[:740]], 1)
+        S.s3_kv_append(cache, first, prompt[:, :K], prompt[:, K:], ws)
+        lists = torch.full((n, K, 6), -7, dtype=torch.int32, device="cuda")
+        out, seen = torch.empty((n, H, D), dtype=torch.bfloat16, device="cuda"), []
+        kept = [(torch.empty_like(lists), torch.empty_like(out)) for _ in range(steps)]
+        torch.cuda.synchronize()
+        for i in range(steps):
+            S.s3_kv_append(cache, batch[i], k[i], v[i], ws)
+            torch.cuda.synchronize() if pause else None
+            S.s3_block_select(cache, batch[i], q[i], 6, ws, blocks=lists)
+            torch.cuda.synchronize() if pause else None
+            S.s3_block_attention(cache, batch[i], q[i], lists, ws, out=out)
+            torch.cuda.synchronize() if pause else None
+            S.s3_block_select(cache, batch[i], q[i - 1], 6, ws, blocks=lists)      # the buffer is written again while the last call ends
+            torch.cuda.synchronize() if pause else None
+            S.s3_block_attention(cache, batch[i], q[i], lists, ws, out=kept[i][1])
+            torch.cuda.synchronize() if pause else None
+            S.s3_block_select(cache, batch[i], q[i], 6, ws, blocks=kept[i][0])
+            torch.cuda.synchronize() if pause else None
+        assert S.s3_workspace_status(ws) == 0
+        return [x for pair in kept for x in pair] + [out, lists, cache.k, cache.v, cache.code, cache.scale]
+
+    want = run(True)
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(run(False), want))
+
+
+def test_masks_of_one_call_are_not_those_of_the_next():
+    """Per-token lists of a chunk as masks, the lists other ones in every call, through one workspace and without a pause."""
+    s = R.Setup([(300, 900)], 8, 8, 128, 64, seed=31)
+    d = Device(s)
+    g = torch.Generator().manual_seed(5)
+    lists = [dev(torch.stack([torch.randperm(15, generator=g)[:7] for _ in range(s.T * 8)]).view(s.T, 8, 7).to(torch.int32)) for _ in range(6)]
+    want = []
+    for x in lists:
+        want.append(S.s3_block_attention(d.cache, d.batch, d.q, x, d.ws)[0])
+        torch.cuda.synchronize()
+    check(s, *S.s3_block_attention(d.cache, d.batch, d.q, lists[0], d.ws, want_lse=True), *R.attention(s, blocks=lists[0].cpu()))
+    for _ in range(3):
+        got = [S.s3_block_attention(d.cache, d.batch, d.q, x, d.ws)[0] for x in lists]
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    d.fine()
