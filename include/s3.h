@@ -568,7 +568,8 @@ s3_status s3_fuse_index_sets(const int32_t* d_centers, int Q, int n_centers, int
  * the call reads must be finite (a zero weight times an infinity is a NaN).
  *
  * All row pitches are in elements, multiples of 8, heads contiguous within a row (a slice of a fused projection will do);
- * pointers 16-byte aligned. One workspace of s3_kv_workspace_bytes() serves every call below.
+ * pointers to rows, pages, summaries, rotation tables and the workspace 16-byte aligned, all others 4-byte (a call refuses what is not). One
+ * workspace of s3_kv_workspace_bytes() serves every call below.
  * ---------------------------------------------------------------------------------------------- */
 typedef struct s3_kv_cache s3_kv_cache;
 typedef struct {

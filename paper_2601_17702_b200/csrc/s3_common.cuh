@@ -26,6 +26,7 @@ s3_status fail(s3_status code, const char* fmt, ...);
         if (!(cond)) return ::s3::fail(code, __VA_ARGS__); \
     } while (0)
 
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 

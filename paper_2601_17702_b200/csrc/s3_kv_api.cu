@@ -199,6 +199,7 @@ s3_status check_batch(const s3_kv_cache* cache, const s3_kv_batch* b)
                (long long)b->ld_pages);
     if (b->T == 0 || b->n_seqs == 0) return S3_OK;
     S3_REQUIRE(b->d_cu_q && b->d_kv_len && b->d_pages, S3_ERR_INVALID_ARG, "null pointer in the batch");
+    S3_REQUIRE(aligned4(b->d_cu_q) && aligned4(b->d_kv_len) && aligned4(b->d_pages), S3_ERR_INVALID_ARG, "misaligned pointer in the batch");
     S3_REQUIRE(static_cast<int64_t>(b->max_kv) <= b->ld_pages * cache->st.d.page_size, S3_ERR_INVALID_ARG,
                "max_kv = %d does not fit %lld table entries of %d positions", b->max_kv, (long long)b->ld_pages, cache->st.d.page_size);
     S3_REQUIRE(b->max_q >= 1 && b->max_q <= b->T, S3_ERR_INVALID_ARG, "max_q = %d out of [1, T = %d]", b->max_q, b->T);
@@ -220,6 +221,13 @@ s3_status check_rows(const char* what, const void* p, int64_t ld, int heads, int
     S3_REQUIRE(ld % 8 == 0 && ld >= static_cast<int64_t>(heads) * dim, S3_ERR_INVALID_ARG,
                "%s: row pitch %lld must be a multiple of 8 and at least %d", what, (long long)ld, heads * dim);
     S3_REQUIRE(ld < (int64_t(1) << 38), S3_ERR_UNSUPPORTED, "%s: row pitch %lld is too large", what, (long long)ld);
+    return S3_OK;
+}
+
+s3_status check_workspace(const void* d_ws, size_t ws_bytes)
+{
+    S3_REQUIRE(d_ws != nullptr && ws_bytes >= S3_WS_HEADER_BYTES, S3_ERR_CAPACITY, "workspace missing or smaller than %d bytes", S3_WS_HEADER_BYTES);
+    S3_REQUIRE(aligned16(d_ws), S3_ERR_INVALID_ARG, "d_ws must be 16-byte aligned");
     return S3_OK;
 }
 
@@ -248,7 +256,8 @@ s3_status attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const vo
     if (b.T == 0 || b.n_seqs == 0) return S3_OK;
     S3_TRY(check_rows("d_q", d_q, ldq, n_heads, c.d.head_dim));
     S3_TRY(check_rows("d_out", d_out, ld_out, n_heads, c.d.head_dim));
-    S3_REQUIRE(d_ws != nullptr && ws_bytes >= S3_WS_HEADER_BYTES, S3_ERR_CAPACITY, "workspace missing or smaller than %d bytes", S3_WS_HEADER_BYTES);
+    S3_REQUIRE(aligned4(d_blocks) && aligned4(d_lse), S3_ERR_INVALID_ARG, "d_blocks or d_lse is misaligned");
+    S3_TRY(check_workspace(d_ws, ws_bytes));
     const int group = n_heads / c.d.n_kv_heads;
     const AttnPlan p = plan_attention(b, group, c.d.n_kv_heads, list_mode, list_mode == LIST_NONE ? b.max_kv : static_cast<int64_t>(s) << c.page_shift,
                                       c.page_shift);
@@ -406,7 +415,8 @@ s3_status s3_kv_append(const s3_kv_cache* cache, const s3_kv_batch* batch, const
     }
     S3_TRY(check_rows("d_k", d_k, ldk, c.d.n_kv_heads, c.d.head_dim));
     S3_TRY(check_rows("d_v", d_v, ldv, c.d.n_kv_heads, c.d.head_dim));
-    S3_REQUIRE(d_ws != nullptr && ws_bytes >= S3_WS_HEADER_BYTES, S3_ERR_CAPACITY, "workspace missing or smaller than %d bytes", S3_WS_HEADER_BYTES);
+    S3_REQUIRE(aligned4(d_positions), S3_ERR_INVALID_ARG, "d_positions is misaligned");
+    S3_TRY(check_workspace(d_ws, ws_bytes));
     return launch_kv_append(c, device_batch(*batch), rope, d_positions, d_q, ldq, n_heads, d_q_out, ld_qo, d_k, ldk, d_v, ldv,
                             static_cast<uint32_t*>(d_ws), static_cast<cudaStream_t>(stream));
 }
@@ -425,8 +435,8 @@ s3_status s3_block_select(const s3_kv_cache* cache, const s3_kv_batch* batch, co
                batch->max_kv, S3_MAX_SELECT_BLOCKS);
     if (batch->T == 0 || batch->n_seqs == 0) return S3_OK;
     S3_TRY(check_rows("d_q", d_q, ldq, n_heads, c.d.head_dim));
-    S3_REQUIRE(d_blocks != nullptr, S3_ERR_INVALID_ARG, "d_blocks is null");
-    S3_REQUIRE(d_ws != nullptr && ws_bytes >= S3_WS_HEADER_BYTES, S3_ERR_CAPACITY, "workspace missing or smaller than %d bytes", S3_WS_HEADER_BYTES);
+    S3_REQUIRE(d_blocks != nullptr && aligned4(d_blocks), S3_ERR_INVALID_ARG, "d_blocks is null or misaligned");
+    S3_TRY(check_workspace(d_ws, ws_bytes));
     return launch_block_select(c, device_batch(*batch), d_q, ldq, n_heads, s, n_first, n_last, d_blocks, static_cast<uint32_t*>(d_ws),
                                static_cast<cudaStream_t>(stream));
 }

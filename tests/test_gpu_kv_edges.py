@@ -5,6 +5,7 @@ Tolerances are those of the tests beside it: eps = 2^-8 (bf16) or 2^-11 (f16); a
 to the type, each off by at most eps of itself, and is rounded once: |out - exact| <= eps (|out| + mean |v|) + 1e-4, the mean of |v|
 under the exact weights. (f16 weights are lifted so that only those 2^-21 and more below the largest are subnormal; what
 these lose is under 2^-32 each, 2^-15 of the largest weight for the 131072 keys here.)"""
+import ctypes as C
 import math
 
 import pytest
@@ -12,6 +13,7 @@ import torch
 
 import kv_reference as R
 import paper_2601_17702_b200 as S
+from paper_2601_17702_b200 import binding as B
 from test_gpu_kv import Device, check, dev
 
 pytestmark = pytest.mark.gpu
@@ -116,4 +118,40 @@ def test_masks_of_one_call_are_not_those_of_the_next():
     for _ in range(3):
         got = [S.s3_block_attention(d.cache, d.batch, d.q, x, d.ws)[0] for x in lists]
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+    d.fine()
+
+
+def test_misaligned_arrays_are_refused_before_any_launch():
+    """A workspace that is a slice at an odd offset, and 4-byte arrays off their boundary, in every call."""
+    s = R.Setup([(1, 4000), (30, 300)], 8, 2, 128, 16, seed=1, outside=0.0)
+    d = Device(s, torch.zeros((s.n_pages, 2, 128), dtype=torch.int8), torch.zeros((s.n_pages, 2)))
+    lists = torch.zeros((s.T, 2, 4), dtype=torch.int32, device="cuda")
+    room = torch.zeros(d.ws.numel() + 64, dtype=torch.uint8, device="cuda")
+    lib, code = B.lib(), S.S3_ERR_INVALID_ARG
+    k, v, out, lse = dev(s.k), dev(s.v), torch.empty_like(d.q), torch.zeros((s.T + 1, 8), device="cuda")
+    params = B.AttnParams(0.1, 1, 0, 0)
+
+    def calls(ws=d.ws, batch=d.batch, lists=lists.data_ptr(), lse=lse.data_ptr(), positions=None):
+        H, D = 8, 128
+        at, n, st = ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream
+        q, o, ref, c = d.q.data_ptr(), out.data_ptr(), C.byref(batch.desc), d.cache.handle
+        cos = torch.ones((4000, 8), device="cuda")
+        rope = S.Rope(cos, cos)
+        return [lib.s3_kv_append(c, ref, rope.ref, positions, None, 0, 0, None, 0, k.data_ptr(), 2 * D, v.data_ptr(), 2 * D, at, n, st),
+                lib.s3_block_select(c, ref, q, H * D, H, 4, 1, 1, lists, at, n, st),
+                lib.s3_paged_attention(c, ref, q, H * D, H, C.byref(params), o, H * D, lse, at, n, st),
+                lib.s3_block_attention(c, ref, q, H * D, H, lists, 4, 2, 1, C.byref(params), o, H * D, lse, at, n, st)]
+
+    assert calls() == [0] * 4
+    for off in (1, 2, 4, 8, 12, 17):
+        assert calls(ws=room[off:]) == [code] * 4
+    assert calls(ws=room[16:]) == [0] * 4 and calls(ws=room[48:]) == [0] * 4
+    assert calls(lists=lists.data_ptr() + 2)[1::2] == [code] * 2
+    assert calls(lse=lse.data_ptr() + 2)[2:] == [code] * 2
+    assert calls(positions=lists.data_ptr() + 1)[0] == code
+    for field in ("d_cu_q", "d_kv_len", "d_pages"):
+        bad = S.KvBatch(d.batch.cu_q, d.batch.kv_len, d.batch.pages, s.T, s.max_q, s.max_kv)
+        setattr(bad.desc, field, getattr(bad.desc, field) + 2)
+        assert calls(batch=bad) == [code] * 4
+    torch.cuda.synchronize()
     d.fine()
