@@ -564,7 +564,8 @@ s3_status s3_fuse_index_sets(const int32_t* d_centers, int Q, int n_centers, int
  * read nor written (it reads as zeros); both are reported through the workspace status as S3_ERR_INVALID_ARG.
  *
  * What a call never uses, whatever it holds (NaN too): positions >= kv_len, pages and blocks that are not listed, table
- * entries past the length. Keys that a row may not see do not enter its result; VALUES at positions < kv_len of a block that
+ * entries past the length, and for attention with a window pages (and their table entries) that lie before the window of
+ * every new row of the sequence. Keys that a row may not see do not enter its result; VALUES at positions < kv_len of a block that
  * the call reads must be finite (a zero weight times an infinity is a NaN).
  *
  * All row pitches are in elements, multiples of 8, heads contiguous within a row (a slice of a fused projection will do);

@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
             const int v = of.v_base + (of.t_lo + t + lane_tile) * TILE + lane_box * box;
             page = pos = -1;
             if (t + lane_tile >= of.t_hi - of.t_lo) return;
-            if (a.list_mode == LIST_NONE) pos = v <= of.it.pos_last ? v : -1;
+            if (a.list_mode == LIST_NONE) pos = v <= of.it.pos_last && v + box > first_seen(a, of.it) ? v : -1;      // boxes before the window are not there
             else if (v < a.s << a.page_shift) {
                 const int id = a.lists[(static_cast<int64_t>(of.it.list) * a.list_heads + (a.list_heads == 1 ? 0 : of.head)) * a.s + (v >> a.page_shift)];
                 // a block all of whose positions are out of sight counts as not listed

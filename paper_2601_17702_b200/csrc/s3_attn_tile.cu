@@ -348,13 +348,16 @@ __global__ void __launch_bounds__(THREADS, 1) tile_kernel(const __grid_constant_
                 if (!some) break;
                 const int n_tiles = g.t_hi - g.t_lo, v_lo = g.v_base + g.t_lo * BN;
                 const int32_t* table = a.b.pages + g.it.seq * a.b.ld_pages;
+                const int gone = first_seen(a, g.it) - box;            // boxes from here and before end before every row's window
                 auto entry = [&](int t, int& page, int& pos) {         // this lane's box of the group of tiles from t
                     page = -1;
                     pos = t + lane / per_tile < n_tiles ? pos_of(g.it, g.head, v_lo + t * BN + lane * box) : -1;
                     if (pos < 0 || pos >= g.it.kv) return;
+                    page = a.n_pages;                                  // beyond the map: reads as zeros
+                    if (pos <= gone) return;
                     const int p = table[pos >> a.page_shift];
-                    page = p < 0 || p >= a.n_pages ? a.n_pages : p;    // beyond the map: reads as zeros
-                    if (page == a.n_pages) dev_set_error(a.status, DEV_BAD_PAGE);
+                    if (p < 0 || p >= a.n_pages) dev_set_error(a.status, DEV_BAD_PAGE);
+                    else page = p;
                 };
                 int t0 = 0, page0, pos0, page1, pos1;                  // groups from t0 and from t0 + group_tiles
                 entry(0, page0, pos0);

@@ -155,3 +155,43 @@ def test_misaligned_arrays_are_refused_before_any_launch():
         assert calls(batch=bad) == [code] * 4
     torch.cuda.synchronize()
     d.fine()
+
+
+def left_behind(s, window):
+    """The setup again, with the pages that no row's window reaches gone: NaN, and no page in the table."""
+    t = R.Setup(s.lens, s.H, s.K, s.D, s.P, s.dtype, seed=s.seed)
+    for i, (n, kv) in enumerate(s.lens):
+        for j in range(max(kv - n - window + 1, 0) // s.P):
+            page = int(t.pages[i, j])
+            t.k_cache[page], t.v_cache[page] = float("nan"), float("nan")
+            t.pages[i, j] = -1 if j % 2 else 2**31 - 1
+    return t
+
+
+@pytest.mark.parametrize("lens", [[(1, 700), (1, 333), (0, 40), (1, 20)], [(3, 1000)], [(90, 700), (3, 500)], [(300, 1500)]])
+@pytest.mark.parametrize("D,P,window,dtype", [(128, 16, 33, torch.bfloat16), (64, 16, 100, torch.float16), (128, 64, 70, torch.bfloat16),
+                                              (64, 128, 1, torch.float16), (128, 32, 200, torch.bfloat16)])
+def test_pages_before_the_window_may_be_gone(lens, D, P, window, dtype):
+    s = R.Setup(lens, 8, 2, D, P, dtype, seed=window)
+    s.seed = window
+    d = Device(left_behind(s, window))
+    out, lse = S.s3_paged_attention(d.cache, d.batch, d.q, d.ws, window=window, want_lse=True)
+    d.fine()
+    check(s, out, lse, *R.attention(s, window=window))
+
+
+@pytest.mark.parametrize("lens", [[(252, 700)] * 3, [(300, 1500)], [(1, 300), (2, 800)]])
+@pytest.mark.parametrize("D,P,n,window,dtype", [(128, 16, 40, 90, torch.bfloat16), (64, 64, 12, 70, torch.float16), (128, 128, 6, 33, torch.float16)])
+def test_listed_pages_before_the_window_may_be_gone(lens, D, P, n, window, dtype):
+    """Per-token lists that name blocks behind the window too, as lists and as masks."""
+    s = R.Setup(lens, 8, 8, D, P, dtype, seed=n)
+    s.seed = n
+    d = Device(left_behind(s, window))
+    g = torch.Generator().manual_seed(n)
+    lists = torch.full((s.T, 1, n), -1, dtype=torch.int32)
+    for t, i, pos in s.rows():
+        blocks = torch.randperm(pos // P + 1, generator=g)[:n]
+        lists[t, 0, :len(blocks)] = blocks.to(torch.int32)
+    out, lse = S.s3_block_attention(d.cache, d.batch, d.q, dev(lists), d.ws, window=window, want_lse=True)
+    d.fine()
+    check(s, out, lse, *R.attention(s, window=window, blocks=lists))
