@@ -654,6 +654,17 @@ s3_status s3_block_attention(const s3_kv_cache* cache, const s3_kv_batch* batch,
                              const int32_t* d_blocks, int s, int list_heads, int per_token, const s3_attn_params* params,
                              void* d_out, int64_t ld_out, float* d_lse /*nullable*/, void* d_ws, size_t ws_bytes, void* stream);
 
+/* How an attention call over a batch of these bounds (n_seqs, T, max_q, max_kv; nothing else of it is looked at) is cut on a device
+ * of n_sms multiprocessors; host arithmetic only. s = 0: s3_paged_attention, else s3_block_attention with lists of s blocks. `tile`:
+ * tiles of 128 query rows, else up to 16 rows at a time; `masked`: lists per token worked on as masks; an item holds up to
+ * tokens_per_item new tokens of a sequence; `blocks` thread blocks take whole items (per key head) or, with `shares`, equal
+ * shares of the keys of all items, whose pieces a second launch joins, after whole_rounds of whole items each. */
+typedef struct {
+    int32_t tile, masked, tokens_per_item, items, blocks, shares, whole_rounds, reserved;
+} s3_attn_plan;
+s3_status s3_attn_plan_describe(const s3_kv_batch* batch, int n_heads, int n_kv_heads, int page_size, int s, int per_token, int n_sms,
+                                s3_attn_plan* out);
+
 #ifdef __cplusplus
 }
 #endif

@@ -38,7 +38,7 @@ EXPORTS = [
     "s3_sae_decode", "s3_head_aggregate_topk", "s3_compact_expand",
     "s3_sae_backward_workspace_bytes", "s3_sae_backward", "s3_adam_update", "s3_cast_f32_to_bf16", "s3_sae_preact",
     "s3_kv_cache_create", "s3_kv_cache_destroy", "s3_kv_workspace_bytes", "s3_kv_append", "s3_block_select", "s3_paged_attention",
-    "s3_block_attention",
+    "s3_block_attention", "s3_attn_plan_describe",
 ]
 
 
@@ -96,6 +96,10 @@ class RopeDesc(C.Structure):
 
 class AttnParams(C.Structure):
     _fields_ = [("scale", C.c_float), ("causal", C.c_int32), ("window", C.c_int32), ("reserved", C.c_int32)]
+
+
+class AttnPlan(C.Structure):
+    _fields_ = [(f, C.c_int32) for f in ("tile", "masked", "tokens_per_item", "items", "blocks", "shares", "whole_rounds", "reserved")]
 
 
 class ScoreParams(C.Structure):
@@ -206,6 +210,7 @@ def lib():
         L.s3_block_select.argtypes = [P, C.POINTER(KvBatchDesc), P, N, I, I, I, I, P, P, C.c_size_t, P]
         L.s3_paged_attention.argtypes = [P, C.POINTER(KvBatchDesc), P, N, I, C.POINTER(AttnParams), P, N, P, P, C.c_size_t, P]
         L.s3_block_attention.argtypes = [P, C.POINTER(KvBatchDesc), P, N, I, P, I, I, I, C.POINTER(AttnParams), P, N, P, P, C.c_size_t, P]
+        L.s3_attn_plan_describe.argtypes = [C.POINTER(KvBatchDesc), I, I, I, I, I, I, C.POINTER(AttnPlan)]
         _lib = L
     return _lib
 
@@ -942,3 +947,12 @@ def s3_block_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, blocks: 
                                     _attn_ref(cache, scale, causal, window), out.data_ptr(), ld_out, lse_ptr, ws.data_ptr(), ws.numel(),
                                     _raw_stream(stream)))
     return out, lse
+
+
+def s3_attn_plan_describe(n_seqs: int, T: int, max_q: int, max_kv: int, n_heads: int, n_kv_heads: int, page_size: int, n_sms: int, s: int = 0,
+                          per_token: bool = True) -> AttnPlan:
+    """How attention over a batch of these bounds is cut on n_sms multiprocessors (s = 0: over the whole cache). Host arithmetic only."""
+    plan = AttnPlan()
+    _check(lib().s3_attn_plan_describe(C.byref(KvBatchDesc(None, None, None, 0, n_seqs, T, max_q, max_kv)), n_heads, n_kv_heads, page_size, s,
+                                       int(per_token), n_sms, C.byref(plan)))
+    return plan

@@ -56,10 +56,10 @@ s3_status make_map(unsigned char (&map)[128], s3_dtype dtype, const void* base, 
 constexpr int kSplitRows = 16;             // rows per item up to which the split kernel serves
 constexpr int kTileRows = 128;
 
-// How an attention call is cut. None of it depends on the device-side lengths.
 // Modelled time of a pair tile under masks, and of the masks themselves and the start (us).
 constexpr double kMaskedTile = 2.7, kMaskedFixed = 12.0;
 
+// How an attention call is cut. None of it depends on the device-side lengths.
 struct AttnPlan {
     bool tile;                             // tile kernel, else split kernel
     bool masked;                           // lists per token as masks over all blocks
@@ -69,9 +69,9 @@ struct AttnPlan {
 
 // Chooses whole units or shares for a plan whose items are set, and returns the modelled time in key tiles. tile_cost: time of one of
 // this plan's key tiles; extra: what shares cost beside their tiles (second launch, partial results, segments cut short).
-double choose_shares(AttnPlan& p, const s3_kv_batch& b, int n_kv_heads, int list_mode, int64_t keys, double tile_cost, double extra)
+double choose_shares(AttnPlan& p, const s3_kv_batch& b, int sms, int n_kv_heads, int list_mode, int64_t keys, double tile_cost, double extra)
 {
-    const int64_t places = (p.tile ? 1 : 2) * static_cast<int64_t>(device_sm_count());     // thread blocks that run at a time
+    const int64_t places = (p.tile ? 1 : 2) * static_cast<int64_t>(sms);     // thread blocks that run at a time
     const int64_t units = static_cast<int64_t>(p.n_items) * n_kv_heads, tiles = (keys + (p.tile ? 127 : 63)) / (p.tile ? 128 : 64);
     // Lists and the items of one sequence are alike: whole units take whole rounds. Sequences of a batch may have any length up to
     // max_kv, which the host does not see: on average taken as 0.6 of it, and whole units end with the longest.
@@ -94,7 +94,7 @@ double choose_shares(AttnPlan& p, const s3_kv_batch& b, int n_kv_heads, int list
 }
 
 // Items of several tokens of a sequence; keys: the most virtual keys an item can have; time: modelled, in key tiles.
-AttnPlan plan_tokens(const s3_kv_batch& b, int group, int n_kv_heads, int list_mode, int64_t keys, double& time)
+AttnPlan plan_tokens(const s3_kv_batch& b, int sms, int group, int n_kv_heads, int list_mode, int64_t keys, double& time)
 {
     AttnPlan p;
     p.masked = false;
@@ -108,11 +108,11 @@ AttnPlan plan_tokens(const s3_kv_batch& b, int group, int n_kv_heads, int list_m
     items(p, one);
     // With one query tile per item the two softmax groups share the keys: a key tile takes a little more than half the time that it
     // takes with two, there are twice as many units, and every key is copied twice as often.
-    time = choose_shares(p, b, n_kv_heads, list_mode, keys, p.tile ? 0.6 : 1.0, p.tile ? 6.0 : 12.0);
+    time = choose_shares(p, b, sms, n_kv_heads, list_mode, keys, p.tile ? 0.6 : 1.0, p.tile ? 6.0 : 12.0);
     if (p.tile && b.max_q > one) {
         AttnPlan q = p;
         items(q, 2 * one);
-        const double pair = choose_shares(q, b, n_kv_heads, list_mode, keys, 1.0, 6.0);
+        const double pair = choose_shares(q, b, sms, n_kv_heads, list_mode, keys, 1.0, 6.0);
         if (pair <= time) {
             p = q;
             time = pair;
@@ -120,6 +120,8 @@ AttnPlan plan_tokens(const s3_kv_batch& b, int group, int n_kv_heads, int list_m
     }
     return p;
 }
+
+int shift_of(int page_size) { return page_size == 16 ? 4 : page_size == 32 ? 5 : page_size == 64 ? 6 : 7; }
 
 int mask_words(const s3_kv_batch& b, int page_shift) { return b.max_kv > 0 ? ((b.max_kv - 1) >> page_shift) / 32 + 1 : 1; }
 
@@ -132,7 +134,7 @@ size_t mask_bytes(const s3_kv_batch& b, int page_shift, int list_heads, int tok_
 }
 
 // keys: the most virtual keys an item can have.
-AttnPlan plan_attention(const s3_kv_batch& b, int group, int n_kv_heads, int list_mode, int64_t keys, int page_shift)
+AttnPlan plan_attention(const s3_kv_batch& b, int sms, int group, int n_kv_heads, int list_mode, int64_t keys, int page_shift)
 {
     AttnPlan p;
     p.masked = false;
@@ -141,14 +143,14 @@ AttnPlan plan_attention(const s3_kv_batch& b, int group, int n_kv_heads, int lis
         p.tok_per_item = 1;
         p.n_items = b.T;
         p.one_item_per_seq = 0;
-        const double listed = choose_shares(p, b, n_kv_heads, list_mode, keys, 1.0, p.tile ? 6.0 : 12.0) * (p.tile ? 2.0 : 0.7);     // us
+        const double listed = choose_shares(p, b, sms, n_kv_heads, list_mode, keys, 1.0, p.tile ? 6.0 : 12.0) * (p.tile ? 2.0 : 0.7);     // us
         // As masks over the blocks that an item lists: a key tile's copies and products serve up to 256 rows, in vain where a row
         // does not list the block, so it pays where the lists are a good part of the context. Measured as lists and as masks, 1024
         // tokens of 4 x 8 heads, 16 random blocks of 64 of each: over 2K keys 325 and 57 us, 8K 325 and 175, 16K 326 and 331, 32K 326
         // and 845; 32 tokens over 2K keys 16.5 and 24.8. The two constants are fitted to these.
         if (static_cast<int64_t>(b.max_q) * group > kSplitRows && mask_words(b, page_shift) <= kMaxMaskWords) {
             double over_all;
-            AttnPlan q = plan_tokens(b, group, n_kv_heads, LIST_NONE, b.max_kv, over_all);
+            AttnPlan q = plan_tokens(b, sms, group, n_kv_heads, LIST_NONE, b.max_kv, over_all);
             if (over_all * kMaskedTile + kMaskedFixed < listed) {
                 p = q;
                 p.masked = true;
@@ -156,7 +158,7 @@ AttnPlan plan_attention(const s3_kv_batch& b, int group, int n_kv_heads, int lis
         }
     } else {
         double time;
-        p = plan_tokens(b, group, n_kv_heads, list_mode, keys, time);
+        p = plan_tokens(b, sms, group, n_kv_heads, list_mode, keys, time);
     }
     p.rows_cap = p.tile ? p.tok_per_item * group : kSplitRows;
     return p;
@@ -207,9 +209,8 @@ s3_status check_batch(const s3_kv_cache* cache, const s3_kv_batch* b)
     return S3_OK;
 }
 
-s3_status check_heads(const s3_kv_cache* cache, int n_heads)
+s3_status check_heads(int n_heads, int k)
 {
-    const int k = cache->st.d.n_kv_heads;
     S3_REQUIRE(n_heads >= 1 && n_heads % k == 0, S3_ERR_INVALID_ARG, "n_heads = %d is not a multiple of %d key heads", n_heads, k);
     S3_REQUIRE(n_heads / k <= S3_MAX_HEAD_GROUP, S3_ERR_UNSUPPORTED, "%d query heads per key head exceed %d", n_heads / k, S3_MAX_HEAD_GROUP);
     return S3_OK;
@@ -247,7 +248,7 @@ s3_status attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const vo
                     int64_t ld_out, float* d_lse, void* d_ws, size_t ws_bytes, void* stream)
 {
     S3_TRY(check_batch(cache, batch));
-    S3_TRY(check_heads(cache, n_heads));
+    S3_TRY(check_heads(n_heads, cache->st.d.n_kv_heads));
     S3_REQUIRE(params != nullptr, S3_ERR_INVALID_ARG, "params is null");
     S3_REQUIRE(isfinite(params->scale) && params->scale > 0.0f, S3_ERR_INVALID_ARG, "scale must be positive and finite");
     S3_REQUIRE(params->window >= 0, S3_ERR_INVALID_ARG, "window = %d is negative", params->window);
@@ -259,7 +260,7 @@ s3_status attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const vo
     S3_REQUIRE(aligned4(d_blocks) && aligned4(d_lse), S3_ERR_INVALID_ARG, "d_blocks or d_lse is misaligned");
     S3_TRY(check_workspace(d_ws, ws_bytes));
     const int group = n_heads / c.d.n_kv_heads;
-    const AttnPlan p = plan_attention(b, group, c.d.n_kv_heads, list_mode, list_mode == LIST_NONE ? b.max_kv : static_cast<int64_t>(s) << c.page_shift,
+    const AttnPlan p = plan_attention(b, device_sm_count(), group, c.d.n_kv_heads, list_mode, list_mode == LIST_NONE ? b.max_kv : static_cast<int64_t>(s) << c.page_shift,
                                       c.page_shift);
 
     AttnArgs a;
@@ -346,7 +347,7 @@ s3_status s3_kv_cache_create(s3_kv_cache** out, const s3_kv_cache_desc* desc)
     s3_kv_cache* c = new (std::nothrow) s3_kv_cache;
     S3_REQUIRE(c != nullptr, S3_ERR_NOMEM, "out of host memory");
     c->st.d = d;
-    c->st.page_shift = d.page_size == 16 ? 4 : d.page_size == 32 ? 5 : d.page_size == 64 ? 6 : 7;
+    c->st.page_shift = shift_of(d.page_size);
     c->st.box_rows = d.page_size < 64 ? d.page_size : 64;
     const uint64_t D = d.head_dim, P = d.page_size;
     const uint64_t K = d.n_kv_heads, N = d.n_pages, ks = d.k_page_stride, vs = d.v_page_stride, half = 64;
@@ -375,7 +376,7 @@ s3_status s3_kv_cache_destroy(s3_kv_cache* cache)
 
 size_t s3_kv_workspace_bytes(const s3_kv_cache* cache, const s3_kv_batch* batch, int n_heads)
 {
-    if (check_batch(cache, batch) != S3_OK || check_heads(cache, n_heads) != S3_OK) return 0;
+    if (check_batch(cache, batch) != S3_OK || check_heads(n_heads, cache->st.d.n_kv_heads) != S3_OK) return 0;
     size_t most = 0;
     if (batch->T > 0 && batch->n_seqs > 0)
         // every call uses at most one of these: the tile kernel's pieces of two query tiles or one, the split kernel's
@@ -390,6 +391,22 @@ size_t s3_kv_workspace_bytes(const s3_kv_cache* cache, const s3_kv_batch* batch,
             if (bytes > most) most = bytes;
         }
     return 256 + most + (batch->T > 0 && batch->n_seqs > 0 ? mask_bytes(*batch, cache->st.page_shift, cache->st.d.n_kv_heads, kTileRows * cache->st.d.n_kv_heads / n_heads) : 0);
+}
+
+s3_status s3_attn_plan_describe(const s3_kv_batch* batch, int n_heads, int n_kv_heads, int page_size, int s, int per_token, int n_sms,
+                                s3_attn_plan* out)
+{
+    S3_REQUIRE(batch != nullptr && out != nullptr, S3_ERR_INVALID_ARG, "batch or out is null");
+    S3_REQUIRE(n_kv_heads >= 1 && n_sms >= 1 && s >= 0, S3_ERR_INVALID_ARG, "n_kv_heads = %d, n_sms = %d, s = %d out of range", n_kv_heads, n_sms, s);
+    S3_TRY(check_heads(n_heads, n_kv_heads));
+    S3_REQUIRE(s <= S3_MAX_BLOCK_LIST, S3_ERR_UNSUPPORTED, "s = %d exceeds %d", s, S3_MAX_BLOCK_LIST);
+    S3_REQUIRE(page_size == 16 || page_size == 32 || page_size == 64 || page_size == 128, S3_ERR_UNSUPPORTED, "page_size = %d (16, 32, 64 or 128)", page_size);
+    S3_REQUIRE(batch->n_seqs >= 1 && batch->max_q >= 1 && batch->max_q <= batch->T && batch->max_kv >= 0, S3_ERR_INVALID_ARG,
+               "n_seqs = %d, T = %d, max_q = %d, max_kv = %d out of range", batch->n_seqs, batch->T, batch->max_q, batch->max_kv);
+    const int shift = shift_of(page_size), mode = s == 0 ? LIST_NONE : per_token ? LIST_PER_TOKEN : LIST_PER_SEQ;
+    const AttnPlan p = plan_attention(*batch, n_sms, n_heads / n_kv_heads, n_kv_heads, mode, s == 0 ? batch->max_kv : static_cast<int64_t>(s) << shift, shift);
+    *out = s3_attn_plan{p.tile, p.masked, p.tok_per_item, p.n_items, p.grid, p.share_min > 0, p.whole_rounds, 0};
+    return S3_OK;
 }
 
 s3_status s3_kv_append(const s3_kv_cache* cache, const s3_kv_batch* batch, const s3_rope* rope, const int32_t* d_positions,
@@ -407,7 +424,7 @@ s3_status s3_kv_append(const s3_kv_cache* cache, const s3_kv_batch* batch, const
             S3_REQUIRE(rope->n_pos >= 1, S3_ERR_INVALID_ARG, "the rotation tables are empty");
         }
     }
-    if (d_q) S3_TRY(check_heads(cache, n_heads));
+    if (d_q) S3_TRY(check_heads(n_heads, cache->st.d.n_kv_heads));
     if (batch->T == 0 || batch->n_seqs == 0) return S3_OK;
     if (d_q) {
         S3_TRY(check_rows("d_q", d_q, ldq, n_heads, c.d.head_dim));
@@ -425,7 +442,7 @@ s3_status s3_block_select(const s3_kv_cache* cache, const s3_kv_batch* batch, co
                           int n_first, int n_last, int32_t* d_blocks, void* d_ws, size_t ws_bytes, void* stream)
 {
     S3_TRY(check_batch(cache, batch));
-    S3_TRY(check_heads(cache, n_heads));
+    S3_TRY(check_heads(n_heads, cache->st.d.n_kv_heads));
     const KvCacheState& c = cache->st;
     S3_REQUIRE(c.d.d_code != nullptr, S3_ERR_STATE, "the cache was created without summaries");
     S3_REQUIRE(s >= 1 && n_first >= 0 && n_last >= 0, S3_ERR_INVALID_ARG, "s = %d, n_first = %d, n_last = %d out of range", s, n_first, n_last);

@@ -195,3 +195,181 @@ def test_listed_pages_before_the_window_may_be_gone(lens, D, P, n, window, dtype
     out, lse = S.s3_block_attention(d.cache, d.batch, d.q, dev(lists), d.ws, window=window, want_lse=True)
     d.fine()
     check(s, out, lse, *R.attention(s, window=window, blocks=lists))
+
+
+@pytest.mark.parametrize("n", [1, 80])
+@pytest.mark.parametrize("offset", [3, 40, 70, 127])
+@pytest.mark.parametrize("octaves", [6, 12, 14.5, 20, 40])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_one_key_far_above_the_others_anywhere_in_a_tile(n, offset, octaves, dtype):
+    """Late tiles in which one key of either half rises over what the weights so far refer to, by less and by more than they hold."""
+    s = R.Setup([(n, 1500)], 4, 1, 128, 16, dtype, seed=int(octaves) + offset)
+    s.q *= 0.1
+    s.q[:, :, 0] = 4.0
+    s.k_cache[..., 0] = s.k_cache[..., 0].nan_to_num(0.0) * 0.1
+    for at, more in ((640 + offset, 0.0), (1024 + offset, 3.0)):
+        page, row = int(s.pages[0, at // 16]), at % 16
+        s.k_cache[page, :, row] = 0
+        s.k_cache[page, :, row, 0] = (octaves + more) * math.log(2.0) / (4 * s.scale)
+    d = Device(s)
+    out, lse = S.s3_paged_attention(d.cache, d.batch, d.q, d.ws, want_lse=True)
+    d.fine()
+    check(s, out, lse, *R.attention(s))
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_wild_keys_out_of_sight_of_few_rows(bad):
+    """A key that only the last two of three rows may see."""
+    s = R.Setup([(3, 200)], 4, 1, 128, 16, seed=8)
+    s.k_cache[int(s.pages[0, 198 // 16]), :, 198 % 16] = bad
+    d = Device(s)
+    out, _ = S.s3_paged_attention(d.cache, d.batch, d.q, d.ws)
+    want, _ = R.attention(s)
+    out = out.double().cpu()
+    assert ((out - want)[:1].abs() <= 2.0 ** -8 * (want[:1].abs() + 1.2) + 1e-4).all()
+    assert torch.isnan(want[1:]).any() and torch.equal(torch.isnan(out[1:]), torch.isnan(want[1:]))
+
+
+# ---- variants of the plan, each with its results -------------------------------------------------
+def on_gpu(s, window=0, blocks=None):
+    """The 64-bit definition on the GPU, a sequence and a query head at a time."""
+    out = torch.zeros((s.T, s.H, s.D), dtype=torch.float64)
+    lse = torch.full((s.T, s.H), -math.inf, dtype=torch.float64)
+    G = s.H // s.K
+    for i, (n, kv) in enumerate(s.lens):
+        if n == 0 or kv == 0:
+            continue
+        rows = slice(s.cu[i], s.cu[i] + n)
+        j, pos = torch.arange(kv, device="cuda"), torch.arange(kv - n, kv, device="cuda")[:, None]
+        base = (j <= pos) & ((j > pos - window) if window else True)
+        for h in range(s.K):
+            k, v = s.held(i, h, "k").cuda(), s.held(i, h, "v").cuda()
+            see = base
+            if blocks is not None:
+                lst = blocks[rows, h if blocks.shape[1] > 1 else 0].cuda().long()
+                last = (kv - 1) // s.P
+                listed = torch.zeros((n, last + 2), dtype=torch.bool, device="cuda")
+                listed.scatter_(1, torch.where((lst >= 0) & (lst <= last), lst, last + 1), True)
+                see = base & listed[:, j // s.P]
+            some = see.any(1, keepdim=True)
+            for g in range(h * G, h * G + G):
+                x = (dev(s.q[rows, g]).double() @ k.T * s.scale).masked_fill(~see, -math.inf)
+                lse[rows, g] = torch.logsumexp(x, -1).cpu()
+                out[rows, g] = (torch.where(some, torch.softmax(x, -1), 0.0) @ v).cpu()
+    return out, lse
+
+
+def variant(s, n=0):
+    """What the plan of this batch picks: (query tiles per item, masks, shares, whole rounds before them)."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    p = S.s3_attn_plan_describe(len(s.lens), s.T, s.max_q, s.max_kv, s.H, s.K, s.P, sms, s=n)
+    tiles = 0 if not p.tile else 2 if p.tokens_per_item > 128 // (s.H // s.K) else 1
+    return tiles, bool(p.masked), bool(p.shares), p.whole_rounds > 0
+
+
+def lists_with_holes(s, n, heads, seed):
+    """n distinct blocks in random places, some ahead of the row or past the sequence, every seventh list empty."""
+    g = torch.Generator().manual_seed(seed)
+    top = torch.tensor([s.lens[i][1] // s.P + 2 for _, i, _ in s.rows()])
+    order = torch.rand((s.T, heads, int(top.max()) + n), generator=g).argsort(-1)[..., :n].to(torch.int32)
+    order[order >= top[:, None, None]] = -1
+    order[torch.arange(s.T) % 7 == 3, 0] = -1
+    return order
+
+
+@pytest.mark.parametrize("lens,H,K,D,P,dtype,window,want", [
+    ([(1, 900), (1, 333)], 8, 2, 128, 16, torch.float16, 0, (0, False, True, False)),
+    ([(2, 60), (1, 33), (0, 9)], 8, 2, 64, 16, torch.bfloat16, 0, (0, False, False, False)),
+    ([(20, 120), (19, 77)], 8, 8, 64, 128, torch.bfloat16, 0, (1, False, False, False)),
+    ([(270, 1621)], 8, 8, 128, 16, torch.float16, 0, (1, False, True, False)),
+    ([(65, 65), (64, 131), (0, 3)] * 4, 28, 4, 128, 32, torch.bfloat16, 40, (2, False, False, False)),
+    ([(270, 1621)], 8, 2, 64, 64, torch.float16, 300, (2, False, True, False)),
+    ([(2401, 9700)], 28, 4, 128, 64, torch.bfloat16, 0, (2, False, True, True)),
+    ([(2399, 9701)], 16, 8, 64, 16, torch.float16, 3000, (2, False, True, True))])
+def test_every_variant_over_the_whole_cache(lens, H, K, D, P, dtype, window, want):
+    s = R.Setup(lens, H, K, D, P, dtype, seed=H + P)
+    assert variant(s) == want
+    d = Device(s)
+    out, lse = S.s3_paged_attention(d.cache, d.batch, d.q, d.ws, window=window, want_lse=True)
+    d.fine()
+    check(s, out, lse, *on_gpu(s, window))
+
+
+@pytest.mark.parametrize("lens,H,K,D,P,n,dtype,window,want", [
+    ([(20, 200), (1, 40)], 8, 8, 128, 16, 4, torch.bfloat16, 0, (0, False, False, False)),
+    ([(20, 200), (1, 40)], 8, 2, 64, 16, 60, torch.float16, 0, (0, False, True, False)),
+    ([(20, 2000), (7, 310)], 20, 1, 128, 16, 20, torch.bfloat16, 0, (1, False, False, False)),
+    ([(20, 4100)], 20, 1, 64, 16, 60, torch.float16, 100, (1, False, True, False)),
+    ([(20, 25), (33, 90)], 8, 8, 64, 64, 40, torch.bfloat16, 0, (1, True, False, False)),
+    ([(270, 1621)], 8, 8, 128, 16, 24, torch.float16, 200, (1, True, True, False)),
+    ([(65, 65), (64, 131), (0, 3)] * 4, 28, 4, 128, 16, 24, torch.float16, 0, (2, True, False, False)),
+    ([(65, 65), (64, 131), (0, 3)] * 4, 28, 4, 64, 16, 24, torch.bfloat16, 40, (2, True, False, False)),
+    ([(252, 565), (251, 400), (0, 60), (252, 252), (3, 500)], 32, 8, 128, 128, 5, torch.bfloat16, 0, (2, True, False, False)),
+    ([(423, 1840), (300, 1500), (77, 1840)], 32, 8, 128, 128, 16, torch.bfloat16, 0, (2, True, True, False)),
+    ([(270, 1621)], 8, 2, 64, 64, 25, torch.float16, 500, (2, True, True, False)),
+    ([(1301, 5303)], 32, 8, 128, 64, 30, torch.bfloat16, 0, (2, True, True, True)),
+    ([(1300, 5302)], 32, 8, 64, 16, 60, torch.float16, 1500, (2, True, True, True))])
+def test_every_variant_of_lists_per_token(lens, H, K, D, P, n, dtype, window, want):
+    s = R.Setup(lens, H, K, D, P, dtype, seed=H + P + n)
+    assert variant(s, n) == want
+    d = Device(s)
+    for heads in {1, K}:
+        lists = lists_with_holes(s, n, heads, seed=n)
+        out, lse = S.s3_block_attention(d.cache, d.batch, d.q, dev(lists), d.ws, window=window, want_lse=True)
+        d.fine()
+        check(s, out, lse, *on_gpu(s, window, lists))
+
+
+def test_the_largest_batchs_workspace_serves_the_others():
+    """Smaller batches in a workspace that a larger one has filled, each with the result that it gets in its own."""
+    big = R.Setup([(300, 4000)], 16, 2, 128, 64, seed=3)
+    d = Device(big)
+    S.s3_paged_attention(d.cache, d.batch, d.q, d.ws)
+    for lens in ([(299, 3000)], [(40, 2500), (3, 500)], [(17, 500)] * 3, [(3, 500)] * 3, [(1, 64)] * 9, [(1, 1)], [(1, 4000)]):
+        s = R.Setup(lens, 16, 2, 128, 64, seed=len(lens), outside=0.0)
+        e = Device(s)
+        assert e.ws.numel() <= d.ws.numel()
+        lists = dev(lists_with_holes(s, 5, 2, seed=1))
+        for ws in (d.ws.fill_(0xFF), e.ws):
+            ws[:S.S3_WS_HEADER_BYTES] = 0
+            got = S.s3_paged_attention(e.cache, e.batch, e.q, ws, want_lse=True) + S.s3_block_attention(e.cache, e.batch, e.q, lists, ws, want_lse=True)
+            assert S.s3_workspace_status(ws) == 0
+            if ws is d.ws:
+                first = got
+        assert all(torch.equal(a, b) for a, b in zip(first, got))
+
+
+@pytest.mark.parametrize("lens,n", [([(1, 3000), (1, 100)], 6), ([(300, 900)], 9), ([(20, 2000), (300, 1621)], 20)])
+def test_a_captured_step_replays_on_new_inputs(lens, n):
+    """Append, select and both attentions in one graph; replayed after the inputs changed in place, it gives what the calls give."""
+    s = R.Setup(lens, 16, 4, 128, 64, seed=15, outside=0.0)
+    d = Device(s, torch.zeros((s.n_pages, 4, 128), dtype=torch.int8), torch.zeros((s.n_pages, 4)))
+    angle = torch.rand((4000, 64), device="cuda") * 6.28
+    rope, k, v = S.Rope(angle.cos(), angle.sin()), dev(s.k), dev(s.v)
+    lists = torch.empty((s.T, 4, n), dtype=torch.int32, device="cuda")
+    rq, a, b = torch.empty_like(d.q), torch.empty_like(d.q), torch.empty_like(d.q)
+    la, lb = (torch.empty((s.T, 16), device="cuda") for _ in range(2))
+
+    def step():
+        S.s3_kv_append(d.cache, d.batch, k, v, d.ws, q=d.q, rope=rope, q_out=rq)
+        S.s3_block_select(d.cache, d.batch, rq, n, d.ws, blocks=lists)
+        S.s3_block_attention(d.cache, d.batch, rq, lists, d.ws, out=a, lse=la)
+        S.s3_paged_attention(d.cache, d.batch, rq, d.ws, out=b, lse=lb)
+
+    def results():
+        return [x.clone() for x in (rq, lists, a, la, b, lb, d.k, d.v, d.code, d.scale)]
+
+    step()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in range(3):
+        for x in (k, v, d.q):
+            x.copy_(x.roll(1, 0) * (1.5 if i == 1 else 1.0))
+        step()
+        want = results()
+        for x in (rq, lists, a, la, b, lb):
+            x.zero_()
+        graph.replay()
+        assert all(torch.equal(x, y) for x, y in zip(results(), want))
+    d.fine()

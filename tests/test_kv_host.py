@@ -1,7 +1,13 @@
 """Paged key / value cache: what holds on the host, without a device."""
 import glob
+import itertools
 import os
 import re
+
+import pytest
+
+import paper_2601_17702_b200 as S
+from paper_2601_17702_b200 import binding as B
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -18,3 +24,34 @@ def test_overlapped_kernels_read_through_the_constant_path_only_what_no_launch_w
         for arg in re.findall(r"__ldg\((.*?)[;,]", text):
             assert "cosv" in arg or "sinv" in arg, f"{os.path.basename(path)}: __ldg({arg}"
     assert found >= 5
+
+
+def test_plans_cover_the_batch():
+    """Items hold every new token, thread blocks no more than run at a time, and masks only where a word per 32 blocks is kept."""
+    seen = set()
+    for sms, (H, K), P, s in itertools.product((1, 148), ((8, 8), (32, 8), (28, 4), (20, 1), (128, 1)), (16, 128), (0, 6, 60)):
+        for n, q, kv in itertools.product((1, 3, 40), (1, 5, 70, 1300), (0, 50, 1000, 9000, 200000)):
+            p = S.s3_attn_plan_describe(n, n * q, q, kv, H, K, P, sms, s=s)
+            assert p.blocks >= 1 and p.blocks <= (1 if p.tile else 2) * sms
+            assert p.items * p.tokens_per_item >= n * q and p.items >= (n * q if s and not p.masked else n)
+            rows = p.tokens_per_item * (H // K)
+            assert p.tokens_per_item >= 1 and rows <= (256 if p.tile else 16)
+            assert p.tile or not p.masked
+            assert not p.masked or (s > 0 and -(-kv // P) <= 128 * 32)
+            assert not p.whole_rounds or (p.shares and p.tile and n == 1 and p.whole_rounds * p.blocks <= p.items * K)
+            seen.add((p.tile, p.masked, p.shares, rows > 128))
+    assert {(0, 0, 0, False), (0, 0, 1, False), (1, 0, 0, False), (1, 0, 1, True), (1, 1, 0, False), (1, 1, 1, True)} <= seen
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(n_heads=9), B.S3_ERR_INVALID_ARG), (dict(n_heads=0), B.S3_ERR_INVALID_ARG), (dict(n_heads=1032), B.S3_ERR_UNSUPPORTED),
+    (dict(n_kv_heads=0), B.S3_ERR_INVALID_ARG), (dict(page_size=48), B.S3_ERR_UNSUPPORTED), (dict(s=513), B.S3_ERR_UNSUPPORTED),
+    (dict(s=-1), B.S3_ERR_INVALID_ARG), (dict(n_sms=0), B.S3_ERR_INVALID_ARG), (dict(max_q=3), B.S3_ERR_INVALID_ARG),
+    (dict(max_q=0), B.S3_ERR_INVALID_ARG), (dict(max_kv=-1), B.S3_ERR_INVALID_ARG), (dict(n_seqs=0), B.S3_ERR_INVALID_ARG)])
+def test_plan_refusals(change, code):
+    args = dict(n_seqs=2, T=2, max_q=1, max_kv=100, n_heads=8, n_kv_heads=8, page_size=64, n_sms=148)
+    S.s3_attn_plan_describe(**args)
+    with pytest.raises(S.S3Error) as e:
+        S.s3_attn_plan_describe(**{**args, **change})
+    assert e.value.code == code
+    assert B.lib().s3_attn_plan_describe(None, 8, 8, 64, 0, 1, 148, None) == B.S3_ERR_INVALID_ARG
