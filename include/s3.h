@@ -545,7 +545,7 @@ s3_status s3_fuse_index_sets(const int32_t* d_centers, int Q, int n_centers, int
  *            (the paper's model side: Alg. 1 Phase 1 runs the LLM over one chunk at a time, Phase 3 answers from the
  *             retained evidence. These calls give a program that attention: over a chunk while it is scanned, over a cache
  *             token by token, and over the evidence blocks only, whether a cheap score picks them per token or the span
- *             retrieval returns them per query. Span width 64 = a page of 64 positions.)
+ *             retrieval returns them per query. Span width 64 = a page of 64 positions. Serving only: no gradients.)
  *
  * Cache: two arrays of n_pages pages, a page [n_kv_heads, page_size, head_dim] contiguous, pages *_page_stride elements
  * apart (so keys and values may interleave page by page in one pool). S3_BF16 or S3_F16; head_dim 64 or 128; page_size
@@ -559,8 +559,8 @@ s3_status s3_fuse_index_sets(const int32_t* d_centers, int Q, int n_centers, int
  * Batch: n_seqs sequences whose new tokens are packed in T rows. Sequence i has rows [d_cu_q[i], d_cu_q[i+1]) (cu_q[0] = 0,
  * cu_q[n_seqs] = T, zero rows allowed), d_kv_len[i] cached positions, its new tokens included and last: its row r
  * has position kv_len - n + r. Block j of the sequence (positions [j, j+1) * page_size) lies in page
- * d_pages[i * ld_pages + j]. max_q / max_kv are host-known upper bounds of new rows / cached positions per sequence;
- * max_kv <= ld_pages * page_size. Lengths outside the bounds are cut to them, and a page outside [0, n_pages) is neither
+ * d_pages[i * ld_pages + j]. max_q / max_kv are host-known upper bounds of new rows / cached positions per sequence,
+ * 1 <= max_q <= T (a fixed bound is cut to the batch's rows) and max_kv <= ld_pages * page_size. Lengths outside the bounds are cut to them, and a page outside [0, n_pages) is neither
  * read nor written (it reads as zeros); both are reported through the workspace status as S3_ERR_INVALID_ARG.
  *
  * What a call never uses, whatever it holds (NaN too): positions >= kv_len, pages and blocks that are not listed, table
@@ -648,7 +648,8 @@ s3_status s3_paged_attention(const s3_kv_cache* cache, const s3_kv_batch* batch,
 /* The same over listed blocks only: d_blocks holds one list of s block numbers per token ([T, list_heads, s], per_token = 1) or
  * per sequence ([n_seqs, list_heads, s], shared by the sequence's new tokens: the layout of the spans that
  * s3_coactivation_score_topspans returns at width = stride = page_size), list_heads being n_kv_heads or 1 (shared by the
- * heads). Any order; entries < 0 or past the sequence's blocks are skipped; a block must not be listed twice.
+ * heads). Any order; entries < 0 or past the sequence's blocks are skipped; a block must not be listed twice (it would count once
+ * or twice, as the plan has it).
  * s <= S3_MAX_BLOCK_LIST. */
 s3_status s3_block_attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const void* d_q, int64_t ldq, int n_heads,
                              const int32_t* d_blocks, int s, int list_heads, int per_token, const s3_attn_params* params,

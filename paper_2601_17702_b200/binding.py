@@ -770,6 +770,7 @@ def s3_sae_preact(sae: "Sae", x: torch.Tensor, out_dtype: torch.dtype = torch.fl
 _KV_DTYPES = {torch.bfloat16: S3_BF16, torch.float16: S3_F16}
 
 
+# These calls serve; no gradient flows through them, whatever their inputs require.
 class KvCache:
     """Handle of a paged key / value cache (s3_kv_cache_create / s3_kv_cache_destroy) over the caller's tensors, which it keeps
     alive: k, v [n_pages, n_kv_heads, page_size, head_dim] bf16 or f16, contiguous within a page (so two views of one pool
