@@ -663,8 +663,8 @@ s3_status s3_block_attention(const s3_kv_cache* cache, const s3_kv_batch* batch,
 typedef struct {
     int32_t tile, masked, tokens_per_item, items, blocks, shares, whole_rounds, reserved;
 } s3_attn_plan;
-s3_status s3_attn_plan_describe(const s3_kv_batch* batch, int n_heads, int n_kv_heads, int page_size, int s, int per_token, int n_sms,
-                                s3_attn_plan* out);
+s3_status s3_attn_plan_describe(const s3_kv_batch* batch, int n_heads, int n_kv_heads, int head_dim, int page_size, int s, int per_token,
+                                int n_sms, s3_attn_plan* out);
 
 #ifdef __cplusplus
 }

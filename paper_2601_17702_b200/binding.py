@@ -210,7 +210,7 @@ def lib():
         L.s3_block_select.argtypes = [P, C.POINTER(KvBatchDesc), P, N, I, I, I, I, P, P, C.c_size_t, P]
         L.s3_paged_attention.argtypes = [P, C.POINTER(KvBatchDesc), P, N, I, C.POINTER(AttnParams), P, N, P, P, C.c_size_t, P]
         L.s3_block_attention.argtypes = [P, C.POINTER(KvBatchDesc), P, N, I, P, I, I, I, C.POINTER(AttnParams), P, N, P, P, C.c_size_t, P]
-        L.s3_attn_plan_describe.argtypes = [C.POINTER(KvBatchDesc), I, I, I, I, I, I, C.POINTER(AttnPlan)]
+        L.s3_attn_plan_describe.argtypes = [C.POINTER(KvBatchDesc), I, I, I, I, I, I, I, C.POINTER(AttnPlan)]
         _lib = L
     return _lib
 
@@ -950,10 +950,10 @@ def s3_block_attention(cache: KvCache, batch: KvBatch, q: torch.Tensor, blocks: 
     return out, lse
 
 
-def s3_attn_plan_describe(n_seqs: int, T: int, max_q: int, max_kv: int, n_heads: int, n_kv_heads: int, page_size: int, n_sms: int, s: int = 0,
-                          per_token: bool = True) -> AttnPlan:
+def s3_attn_plan_describe(n_seqs: int, T: int, max_q: int, max_kv: int, n_heads: int, n_kv_heads: int, head_dim: int, page_size: int, n_sms: int,
+                          s: int = 0, per_token: bool = True) -> AttnPlan:
     """How attention over a batch of these bounds is cut on n_sms multiprocessors (s = 0: over the whole cache). Host arithmetic only."""
     plan = AttnPlan()
-    _check(lib().s3_attn_plan_describe(C.byref(KvBatchDesc(None, None, None, 0, n_seqs, T, max_q, max_kv)), n_heads, n_kv_heads, page_size, s,
-                                       int(per_token), n_sms, C.byref(plan)))
+    _check(lib().s3_attn_plan_describe(C.byref(KvBatchDesc(None, None, None, 0, n_seqs, T, max_q, max_kv)), n_heads, n_kv_heads, head_dim, page_size,
+                                       s, int(per_token), n_sms, C.byref(plan)))
     return plan

@@ -59,6 +59,14 @@ constexpr int kTileRows = 128;
 // Modelled time of a pair tile under masks, and of the masks themselves and the start (us).
 constexpr double kMaskedTile = 2.7, kMaskedFixed = 12.0;
 
+// Keys and values of a sequence from which whole rounds go before shares (bytes), see choose_shares.
+constexpr int64_t kRoundsBytes = 76000000;
+
+// What a plan depends on beside the batch's bounds.
+struct PlanShape {
+    int sms, group, n_kv_heads, head_dim, page_shift;
+};
+
 // How an attention call is cut. None of it depends on the device-side lengths.
 struct AttnPlan {
     bool tile;                             // tile kernel, else split kernel
@@ -69,10 +77,10 @@ struct AttnPlan {
 
 // Chooses whole units or shares for a plan whose items are set, and returns the modelled time in key tiles. tile_cost: time of one of
 // this plan's key tiles; extra: what shares cost beside their tiles (second launch, partial results, segments cut short).
-double choose_shares(AttnPlan& p, const s3_kv_batch& b, int sms, int n_kv_heads, int list_mode, int64_t keys, double tile_cost, double extra)
+double choose_shares(AttnPlan& p, const s3_kv_batch& b, const PlanShape& c, int list_mode, int64_t keys, double tile_cost, double extra)
 {
-    const int64_t places = (p.tile ? 1 : 2) * static_cast<int64_t>(sms);     // thread blocks that run at a time
-    const int64_t units = static_cast<int64_t>(p.n_items) * n_kv_heads, tiles = (keys + (p.tile ? 127 : 63)) / (p.tile ? 128 : 64);
+    const int64_t places = (p.tile ? 1 : 2) * static_cast<int64_t>(c.sms);     // thread blocks that run at a time
+    const int64_t units = static_cast<int64_t>(p.n_items) * c.n_kv_heads, tiles = (keys + (p.tile ? 127 : 63)) / (p.tile ? 128 : 64);
     // Lists and the items of one sequence are alike: whole units take whole rounds. Sequences of a batch may have any length up to
     // max_kv, which the host does not see: on average taken as 0.6 of it, and whole units end with the longest.
     const bool alike = list_mode != LIST_NONE || b.n_seqs == 1;
@@ -87,19 +95,24 @@ double choose_shares(AttnPlan& p, const s3_kv_batch& b, int sms, int n_kv_heads,
     }
     p.grid = static_cast<int>(places);
     p.share_min = p.tile ? 2 : 4;
-    // A chunk late in a prompt: units of nearly equal length. Whole rounds of them go first, all blocks sweeping the keys in step, and
-    // only the rest is shared: the blocks of a key head then read the same tiles at the same time.
-    if (p.tile && list_mode == LIST_NONE && b.n_seqs == 1 && b.max_kv >= 4 * static_cast<int64_t>(b.max_q)) p.whole_rounds = static_cast<int>(units / places);
+    // A chunk late in a prompt: units of nearly equal length. Whole rounds of them may go first, all blocks sweeping the keys in step, and
+    // only the rest be shared: the blocks of a key head then read the same tiles at the same time, which counts once the keys and
+    // values of the sequence no longer stay in the L2 cache. Shares only and with rounds, from rest, 2048 tokens of 4 x 8 heads of 128:
+    // over 9000 keys (37 MB) 251 and 262 us, 16384 (67 MB) 432 and 438, 20000 (82 MB) 535 and 530, 24000 (98 MB) 653 and 626, 32768
+    // (134 MB) 929 and 846; 2700 tokens of 7 x 4 heads over 11000 (23 MB) 336 and 367, over 65536 (134 MB) 2116 and 1961.
+    if (p.tile && list_mode == LIST_NONE && b.n_seqs == 1 && b.max_kv >= 4 * static_cast<int64_t>(b.max_q) &&
+        static_cast<int64_t>(b.max_kv) * c.n_kv_heads * c.head_dim * 4 >= kRoundsBytes)
+        p.whole_rounds = static_cast<int>(units / places);
     return share;
 }
 
 // Items of several tokens of a sequence; keys: the most virtual keys an item can have; time: modelled, in key tiles.
-AttnPlan plan_tokens(const s3_kv_batch& b, int sms, int group, int n_kv_heads, int list_mode, int64_t keys, double& time)
+AttnPlan plan_tokens(const s3_kv_batch& b, const PlanShape& c, int list_mode, int64_t keys, double& time)
 {
     AttnPlan p;
     p.masked = false;
-    p.tile = static_cast<int64_t>(b.max_q) * group > kSplitRows;
-    const int one = (p.tile ? kTileRows : kSplitRows) / group;
+    p.tile = static_cast<int64_t>(b.max_q) * c.group > kSplitRows;
+    const int one = (p.tile ? kTileRows : kSplitRows) / c.group;
     auto items = [&](AttnPlan& q, int tokens) {
         q.tok_per_item = tokens;
         q.one_item_per_seq = b.max_q <= tokens;
@@ -108,11 +121,11 @@ AttnPlan plan_tokens(const s3_kv_batch& b, int sms, int group, int n_kv_heads, i
     items(p, one);
     // With one query tile per item the two softmax groups share the keys: a key tile takes a little more than half the time that it
     // takes with two, there are twice as many units, and every key is copied twice as often.
-    time = choose_shares(p, b, sms, n_kv_heads, list_mode, keys, p.tile ? 0.6 : 1.0, p.tile ? 6.0 : 12.0);
+    time = choose_shares(p, b, c, list_mode, keys, p.tile ? 0.6 : 1.0, p.tile ? 6.0 : 12.0);
     if (p.tile && b.max_q > one) {
         AttnPlan q = p;
         items(q, 2 * one);
-        const double pair = choose_shares(q, b, sms, n_kv_heads, list_mode, keys, 1.0, 6.0);
+        const double pair = choose_shares(q, b, c, list_mode, keys, 1.0, 6.0);
         if (pair <= time) {
             p = q;
             time = pair;
@@ -134,23 +147,23 @@ size_t mask_bytes(const s3_kv_batch& b, int page_shift, int list_heads, int tok_
 }
 
 // keys: the most virtual keys an item can have.
-AttnPlan plan_attention(const s3_kv_batch& b, int sms, int group, int n_kv_heads, int list_mode, int64_t keys, int page_shift)
+AttnPlan plan_attention(const s3_kv_batch& b, const PlanShape& c, int list_mode, int64_t keys)
 {
     AttnPlan p;
     p.masked = false;
     if (list_mode == LIST_PER_TOKEN) {
-        p.tile = group > kSplitRows;
+        p.tile = c.group > kSplitRows;
         p.tok_per_item = 1;
         p.n_items = b.T;
         p.one_item_per_seq = 0;
-        const double listed = choose_shares(p, b, sms, n_kv_heads, list_mode, keys, 1.0, p.tile ? 6.0 : 12.0) * (p.tile ? 2.0 : 0.7);     // us
+        const double listed = choose_shares(p, b, c, list_mode, keys, 1.0, p.tile ? 6.0 : 12.0) * (p.tile ? 2.0 : 0.7);     // us
         // As masks over the blocks that an item lists: a key tile's copies and products serve up to 256 rows, in vain where a row
         // does not list the block, so it pays where the lists are a good part of the context. Measured as lists and as masks, 1024
         // tokens of 4 x 8 heads, 16 random blocks of 64 of each: over 2K keys 325 and 57 us, 8K 325 and 175, 16K 326 and 331, 32K 326
         // and 845; 32 tokens over 2K keys 16.5 and 24.8. The two constants are fitted to these.
-        if (static_cast<int64_t>(b.max_q) * group > kSplitRows && mask_words(b, page_shift) <= kMaxMaskWords) {
+        if (static_cast<int64_t>(b.max_q) * c.group > kSplitRows && mask_words(b, c.page_shift) <= kMaxMaskWords) {
             double over_all;
-            AttnPlan q = plan_tokens(b, sms, group, n_kv_heads, LIST_NONE, b.max_kv, over_all);
+            AttnPlan q = plan_tokens(b, c, LIST_NONE, b.max_kv, over_all);
             if (over_all * kMaskedTile + kMaskedFixed < listed) {
                 p = q;
                 p.masked = true;
@@ -158,9 +171,9 @@ AttnPlan plan_attention(const s3_kv_batch& b, int sms, int group, int n_kv_heads
         }
     } else {
         double time;
-        p = plan_tokens(b, sms, group, n_kv_heads, list_mode, keys, time);
+        p = plan_tokens(b, c, list_mode, keys, time);
     }
-    p.rows_cap = p.tile ? p.tok_per_item * group : kSplitRows;
+    p.rows_cap = p.tile ? p.tok_per_item * c.group : kSplitRows;
     return p;
 }
 
@@ -260,8 +273,8 @@ s3_status attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const vo
     S3_REQUIRE(aligned4(d_blocks) && aligned4(d_lse), S3_ERR_INVALID_ARG, "d_blocks or d_lse is misaligned");
     S3_TRY(check_workspace(d_ws, ws_bytes));
     const int group = n_heads / c.d.n_kv_heads;
-    const AttnPlan p = plan_attention(b, device_sm_count(), group, c.d.n_kv_heads, list_mode, list_mode == LIST_NONE ? b.max_kv : static_cast<int64_t>(s) << c.page_shift,
-                                      c.page_shift);
+    const AttnPlan p = plan_attention(b, PlanShape{device_sm_count(), group, c.d.n_kv_heads, c.d.head_dim, c.page_shift}, list_mode,
+                                      list_mode == LIST_NONE ? b.max_kv : static_cast<int64_t>(s) << c.page_shift);
 
     AttnArgs a;
     memset(&a, 0, sizeof(a));
@@ -393,18 +406,20 @@ size_t s3_kv_workspace_bytes(const s3_kv_cache* cache, const s3_kv_batch* batch,
     return 256 + most + (batch->T > 0 && batch->n_seqs > 0 ? mask_bytes(*batch, cache->st.page_shift, cache->st.d.n_kv_heads, kTileRows * cache->st.d.n_kv_heads / n_heads) : 0);
 }
 
-s3_status s3_attn_plan_describe(const s3_kv_batch* batch, int n_heads, int n_kv_heads, int page_size, int s, int per_token, int n_sms,
-                                s3_attn_plan* out)
+s3_status s3_attn_plan_describe(const s3_kv_batch* batch, int n_heads, int n_kv_heads, int head_dim, int page_size, int s, int per_token,
+                                int n_sms, s3_attn_plan* out)
 {
     S3_REQUIRE(batch != nullptr && out != nullptr, S3_ERR_INVALID_ARG, "batch or out is null");
     S3_REQUIRE(n_kv_heads >= 1 && n_sms >= 1 && s >= 0, S3_ERR_INVALID_ARG, "n_kv_heads = %d, n_sms = %d, s = %d out of range", n_kv_heads, n_sms, s);
     S3_TRY(check_heads(n_heads, n_kv_heads));
     S3_REQUIRE(s <= S3_MAX_BLOCK_LIST, S3_ERR_UNSUPPORTED, "s = %d exceeds %d", s, S3_MAX_BLOCK_LIST);
+    S3_REQUIRE(head_dim == 64 || head_dim == 128, S3_ERR_UNSUPPORTED, "head_dim = %d (64 or 128)", head_dim);
     S3_REQUIRE(page_size == 16 || page_size == 32 || page_size == 64 || page_size == 128, S3_ERR_UNSUPPORTED, "page_size = %d (16, 32, 64 or 128)", page_size);
     S3_REQUIRE(batch->n_seqs >= 1 && batch->max_q >= 1 && batch->max_q <= batch->T && batch->max_kv >= 0, S3_ERR_INVALID_ARG,
                "n_seqs = %d, T = %d, max_q = %d, max_kv = %d out of range", batch->n_seqs, batch->T, batch->max_q, batch->max_kv);
     const int shift = shift_of(page_size), mode = s == 0 ? LIST_NONE : per_token ? LIST_PER_TOKEN : LIST_PER_SEQ;
-    const AttnPlan p = plan_attention(*batch, n_sms, n_heads / n_kv_heads, n_kv_heads, mode, s == 0 ? batch->max_kv : static_cast<int64_t>(s) << shift, shift);
+    const AttnPlan p = plan_attention(*batch, PlanShape{n_sms, n_heads / n_kv_heads, n_kv_heads, head_dim, shift}, mode,
+                                      s == 0 ? batch->max_kv : static_cast<int64_t>(s) << shift);
     *out = s3_attn_plan{p.tile, p.masked, p.tok_per_item, p.n_items, p.grid, p.share_min > 0, p.whole_rounds, 0};
     return S3_OK;
 }

@@ -262,7 +262,7 @@ def on_gpu(s, window=0, blocks=None):
 def variant(s, n=0):
     """What the plan of this batch picks: (query tiles per item, masks, shares, whole rounds before them)."""
     sms = torch.cuda.get_device_properties(0).multi_processor_count
-    p = S.s3_attn_plan_describe(len(s.lens), s.T, s.max_q, s.max_kv, s.H, s.K, s.P, sms, s=n)
+    p = S.s3_attn_plan_describe(len(s.lens), s.T, s.max_q, s.max_kv, s.H, s.K, s.D, s.P, sms, s=n)
     tiles = 0 if not p.tile else 2 if p.tokens_per_item > 128 // (s.H // s.K) else 1
     return tiles, bool(p.masked), bool(p.shares), p.whole_rounds > 0
 
@@ -284,8 +284,9 @@ def lists_with_holes(s, n, heads, seed):
     ([(270, 1621)], 8, 8, 128, 16, torch.float16, 0, (1, False, True, False)),
     ([(65, 65), (64, 131), (0, 3)] * 4, 28, 4, 128, 32, torch.bfloat16, 40, (2, False, False, False)),
     ([(270, 1621)], 8, 2, 64, 64, torch.float16, 300, (2, False, True, False)),
-    ([(2401, 9700)], 28, 4, 128, 64, torch.bfloat16, 0, (2, False, True, True)),
-    ([(2399, 9701)], 16, 8, 64, 16, torch.float16, 3000, (2, False, True, True))])
+    ([(2401, 9700)], 28, 4, 128, 64, torch.bfloat16, 0, (2, False, True, False)),
+    ([(2561, 10301)], 16, 16, 128, 64, torch.bfloat16, 0, (2, False, True, True)),
+    ([(1299, 9401)], 32, 32, 64, 16, torch.float16, 3000, (2, False, True, True))])
 def test_every_variant_over_the_whole_cache(lens, H, K, D, P, dtype, window, want):
     s = R.Setup(lens, H, K, D, P, dtype, seed=H + P)
     assert variant(s) == want
@@ -307,8 +308,8 @@ def test_every_variant_over_the_whole_cache(lens, H, K, D, P, dtype, window, wan
     ([(252, 565), (251, 400), (0, 60), (252, 252), (3, 500)], 32, 8, 128, 128, 5, torch.bfloat16, 0, (2, True, False, False)),
     ([(423, 1840), (300, 1500), (77, 1840)], 32, 8, 128, 128, 16, torch.bfloat16, 0, (2, True, True, False)),
     ([(270, 1621)], 8, 2, 64, 64, 25, torch.float16, 500, (2, True, True, False)),
-    ([(1301, 5303)], 32, 8, 128, 64, 30, torch.bfloat16, 0, (2, True, True, True)),
-    ([(1300, 5302)], 32, 8, 64, 16, 60, torch.float16, 1500, (2, True, True, True))])
+    ([(2601, 10405)], 16, 16, 128, 64, 30, torch.bfloat16, 0, (2, True, True, True)),
+    ([(1300, 9402)], 32, 32, 64, 16, 60, torch.float16, 1500, (2, True, True, True))])
 def test_every_variant_of_lists_per_token(lens, H, K, D, P, n, dtype, window, want):
     s = R.Setup(lens, H, K, D, P, dtype, seed=H + P + n)
     assert variant(s, n) == want

@@ -31,27 +31,36 @@ def test_plans_cover_the_batch():
     seen = set()
     for sms, (H, K), P, s in itertools.product((1, 148), ((8, 8), (32, 8), (28, 4), (20, 1), (128, 1)), (16, 128), (0, 6, 60)):
         for n, q, kv in itertools.product((1, 3, 40), (1, 5, 70, 1300), (0, 50, 1000, 9000, 200000)):
-            p = S.s3_attn_plan_describe(n, n * q, q, kv, H, K, P, sms, s=s)
+            p = S.s3_attn_plan_describe(n, n * q, q, kv, H, K, 128, P, sms, s=s)
             assert p.blocks >= 1 and p.blocks <= (1 if p.tile else 2) * sms
             assert p.items * p.tokens_per_item >= n * q and p.items >= (n * q if s and not p.masked else n)
             rows = p.tokens_per_item * (H // K)
             assert p.tokens_per_item >= 1 and rows <= (256 if p.tile else 16)
             assert p.tile or not p.masked
             assert not p.masked or (s > 0 and -(-kv // P) <= 128 * 32)
-            assert not p.whole_rounds or (p.shares and p.tile and n == 1 and p.whole_rounds * p.blocks <= p.items * K)
+            assert not p.whole_rounds or (kv * K * 512 > 7e7 and p.shares and p.tile and n == 1 and p.whole_rounds * p.blocks <= p.items * K)
             seen.add((p.tile, p.masked, p.shares, rows > 128))
     assert {(0, 0, 0, False), (0, 0, 1, False), (1, 0, 0, False), (1, 0, 1, True), (1, 1, 0, False), (1, 1, 1, True)} <= seen
 
 
 @pytest.mark.parametrize("change,code", [
     (dict(n_heads=9), B.S3_ERR_INVALID_ARG), (dict(n_heads=0), B.S3_ERR_INVALID_ARG), (dict(n_heads=1032), B.S3_ERR_UNSUPPORTED),
-    (dict(n_kv_heads=0), B.S3_ERR_INVALID_ARG), (dict(page_size=48), B.S3_ERR_UNSUPPORTED), (dict(s=513), B.S3_ERR_UNSUPPORTED),
+    (dict(n_kv_heads=0), B.S3_ERR_INVALID_ARG), (dict(page_size=48), B.S3_ERR_UNSUPPORTED), (dict(head_dim=96), B.S3_ERR_UNSUPPORTED), (dict(s=513), B.S3_ERR_UNSUPPORTED),
     (dict(s=-1), B.S3_ERR_INVALID_ARG), (dict(n_sms=0), B.S3_ERR_INVALID_ARG), (dict(max_q=3), B.S3_ERR_INVALID_ARG),
     (dict(max_q=0), B.S3_ERR_INVALID_ARG), (dict(max_kv=-1), B.S3_ERR_INVALID_ARG), (dict(n_seqs=0), B.S3_ERR_INVALID_ARG)])
 def test_plan_refusals(change, code):
-    args = dict(n_seqs=2, T=2, max_q=1, max_kv=100, n_heads=8, n_kv_heads=8, page_size=64, n_sms=148)
+    args = dict(n_seqs=2, T=2, max_q=1, max_kv=100, n_heads=8, n_kv_heads=8, head_dim=64, page_size=64, n_sms=148)
     S.s3_attn_plan_describe(**args)
     with pytest.raises(S.S3Error) as e:
         S.s3_attn_plan_describe(**{**args, **change})
     assert e.value.code == code
-    assert B.lib().s3_attn_plan_describe(None, 8, 8, 64, 0, 1, 148, None) == B.S3_ERR_INVALID_ARG
+    assert B.lib().s3_attn_plan_describe(None, 8, 8, 64, 64, 0, 1, 148, None) == B.S3_ERR_INVALID_ARG
+
+
+def test_whole_rounds_go_before_shares_only_past_the_cache():
+    """One late chunk: in step where its keys and values exceed what the L2 cache holds of them, in shares alone where they do not."""
+    rounds = lambda q, kv, H, K, D: S.s3_attn_plan_describe(1, q, q, kv, H, K, D, 64, 148).whole_rounds
+    assert [rounds(2048, kv, 32, 8, 128) for kv in (9000, 16384, 20000, 32768)] == [0, 0, 1, 1]
+    assert rounds(2700, 11000, 28, 4, 128) == 0 and rounds(2700, 65536, 28, 4, 128) == 2
+    assert rounds(2048, 32768, 32, 8, 64) == 0 and rounds(2048, 65536, 32, 8, 64) == 1
+    assert rounds(8192, 20000, 32, 8, 128) == 0
