@@ -551,6 +551,7 @@ template <class T, int D>
 s3_status launch_rows(const KvCacheState& c, const AttnArgs& a, cudaStream_t stream)
 {
     const int rows = (a.list_mode == LIST_PER_TOKEN ? 1 : a.b.max_q) * a.group;       // of the largest item
+    // one group of 8 query rows or two (us, up to 8 rows): one token over 131072 keys 93 and 97, over 777 13.7 and 16.7; lists 328 and 466
     return rows <= 8 ? launch_split<T, D, 1>(c, a, stream) : launch_split<T, D, 2>(c, a, stream);
 }
 

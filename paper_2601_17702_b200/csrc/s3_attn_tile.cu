@@ -18,9 +18,10 @@
 // stays inside the type, see WeightRange, and the sum in fp32); the MMA order makes S(j+1) complete
 // only after O += P(j) V(j), so the group may touch O as soon as it sees the next S.
 //
-// Measured: 2048 tokens of 4 x 8 heads at the end of 32768 keys in 909 to 963 us (1.11 to 1.17 PFLOP/s; 1.63 is what a large library
-// product reaches here), with the tensor pipe busy 62 % and that of the exponentials 65 % of the time; 7 ragged chunks of up to 733
-// tokens at head_dim 64 72 us, where the units' starts and ends show.
+// Measured: 2048 tokens of 4 x 8 heads at the end of 32768 keys in 840 us from rest (1.27 PFLOP/s; 1.63 is what a large library product
+// reaches here) and 940 to 985 us back to back, when the power limit holds the clock down (1.08 to 1.13; the product 1.38 then), with
+// the tensor pipe busy 62 % and that of the exponentials 65 % of the time; 7 ragged chunks of up to 733 tokens at head_dim 64
+// 72 us, where the units' starts and ends show.
 //
 // Every mbarrier wait is bounded; one that runs out sets the status word and the block's abort flag, and the block waits for its
 // copies and frees its tensor memory before it leaves.

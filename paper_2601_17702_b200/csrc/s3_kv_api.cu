@@ -53,7 +53,10 @@ s3_status make_map(unsigned char (&map)[128], s3_dtype dtype, const void* base, 
     return S3_OK;
 }
 
-constexpr int kSplitRows = 16;             // rows per item up to which the split kernel serves
+// Rows per item up to which the split kernel serves (its registers hold 16). Split and tile kernel there, keys times 8 heads of 128: one
+// row over 131072 keys times 4 heads 92 and 105 us, 32 sequences of 16 rows over 8192 176 and 191, over 2000 62 and 86, 64 over 700
+// 52 and 92, one over 777 20.1 and 19.5; lists per token, 64 tokens of 8 heads 30 and 71, of 16 heads 42 and 71.
+constexpr int kSplitRows = 16;
 constexpr int kTileRows = 128;
 
 // Modelled time of a pair tile under masks, and of the masks themselves and the start (us).
@@ -76,13 +79,20 @@ struct AttnPlan {
 };
 
 // Chooses whole units or shares for a plan whose items are set, and returns the modelled time in key tiles. tile_cost: time of one of
-// this plan's key tiles; extra: what shares cost beside their tiles (second launch, partial results, segments cut short).
+// this plan's key tiles; extra: what shares cost beside their tiles (second launch, partial results, segments cut short): 12 tiles of
+// the split kernel, 6 of the tile kernel. Whole and shares measured (us, 4 x 8 heads of 128):
+//   split, lists of 16 blocks of 64, of 8 sequences 16.8 and 15.0, of 16 19.6 and 23.9, 24 24.7 and 28.9, 36 31.9 and 33.4, 48 (two rounds)
+//   43.7 and 46.3; one row over 500 keys 10.4 and 11.7, 777 13.1 and 13.5, 1500 18.5 and 12.4, 6000 57 and 16;
+//   tile, one query tile, 64 tokens over 500 keys 15.9 and 20.4, 1000 20.3 and 20.7, 2000 29.9 and 23.3; 256 over 4000 49 and 42; 512 over
+//   4000 51 and 58; two query tiles, 4 x 128 over 1000 27.5 and 33.6, 4 x 128 over 3000 57 and 55, 8 x 128 over 3000 108 and 80.
 double choose_shares(AttnPlan& p, const s3_kv_batch& b, const PlanShape& c, int list_mode, int64_t keys, double tile_cost, double extra)
 {
     const int64_t places = (p.tile ? 1 : 2) * static_cast<int64_t>(c.sms);     // thread blocks that run at a time
     const int64_t units = static_cast<int64_t>(p.n_items) * c.n_kv_heads, tiles = (keys + (p.tile ? 127 : 63)) / (p.tile ? 128 : 64);
     // Lists and the items of one sequence are alike: whole units take whole rounds. Sequences of a batch may have any length up to
-    // max_kv, which the host does not see: on average taken as 0.6 of it, and whole units end with the longest.
+    // max_kv, which the host does not see: on average taken as 0.6 of it, and whole units end with the longest. Whole and shares, one
+    // row each: 24 sequences of up to 4000 keys 48.6 and 43.5, 16 43.5 and 34.6, 80 (three rounds) 141 and 117. Where they are all of
+    // the bound's length the guess loses: 24 of 2000 35.6 and 42.2 (taken), 16 chunks of 64 tokens over 4000 78 and 101 (taken).
     const bool alike = list_mode != LIST_NONE || b.n_seqs == 1;
     const int64_t rounds = (units + places - 1) / places;
     const double whole = alike || rounds <= 1 ? static_cast<double>(rounds * tiles) * tile_cost : 1e30;
@@ -94,6 +104,8 @@ double choose_shares(AttnPlan& p, const s3_kv_batch& b, const PlanShape& c, int 
         return whole;
     }
     p.grid = static_cast<int>(places);
+    // A share has at least this many tiles, or the join has more pieces than it saves. Least shares of 1, 2, 4, 8 tiles: split, one row
+    // over 777 keys 11.1, 13.1, 13.3, 16.2, over 3000 14.5, 14.5, 14.8, 17.2; of 1, 2, 4: tile, 64 tokens over 1000 23.4, 23.5, 25.8.
     p.share_min = p.tile ? 2 : 4;
     // A chunk late in a prompt: units of nearly equal length. Whole rounds of them may go first, all blocks sweeping the keys in step, and
     // only the rest be shared: the blocks of a key head then read the same tiles at the same time, which counts once the keys and
@@ -120,7 +132,9 @@ AttnPlan plan_tokens(const s3_kv_batch& b, const PlanShape& c, int list_mode, in
     };
     items(p, one);
     // With one query tile per item the two softmax groups share the keys: a key tile takes a little more than half the time that it
-    // takes with two, there are twice as many units, and every key is copied twice as often.
+    // takes with two, there are twice as many units, and every key is copied twice as often. One and two, 4 x 8 heads of 128: 512
+    // tokens over 1000 keys 20.7 and 26.5, 1 x 64 over 2000 23.3 and 25.9; 4 x 128 over 1000 34 and 27.5, 16 x 64 over 1000 55 and 33, 8 x 128
+    // over 3000 94 and 80.
     time = choose_shares(p, b, c, list_mode, keys, p.tile ? 0.6 : 1.0, p.tile ? 6.0 : 12.0);
     if (p.tile && b.max_q > one) {
         AttnPlan q = p;
@@ -160,7 +174,9 @@ AttnPlan plan_attention(const s3_kv_batch& b, const PlanShape& c, int list_mode,
         // As masks over the blocks that an item lists: a key tile's copies and products serve up to 256 rows, in vain where a row
         // does not list the block, so it pays where the lists are a good part of the context. Measured as lists and as masks, 1024
         // tokens of 4 x 8 heads, 16 random blocks of 64 of each: over 2K keys 325 and 57 us, 8K 325 and 175, 16K 326 and 331, 32K 326
-        // and 845; 32 tokens over 2K keys 16.5 and 24.8. The two constants are fitted to these.
+        // and 845; 32 tokens over 2K keys 16.5 and 24.8. The two constants are fitted to these and know neither head_dim nor page size:
+        // with 8 blocks of 128 over 8K keys 322 and 177, 24 blocks of 16 184 and 247, 16 of 64 at head_dim 64 299 and 157, 600 tokens of 7 x 4
+        // heads over 4K 107 and 73, 300 of 4 x 4 heads of 64 with 24 blocks of 16 over 4K 32.9 and 40.2, each the faster one taken.
         if (static_cast<int64_t>(b.max_q) * c.group > kSplitRows && mask_words(b, c.page_shift) <= kMaxMaskWords) {
             double over_all;
             AttnPlan q = plan_tokens(b, c, LIST_NONE, b.max_kv, over_all);
