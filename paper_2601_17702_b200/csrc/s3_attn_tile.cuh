@@ -948,8 +948,10 @@ __global__ void __launch_bounds__(threads_of(I8, FORM), 1) tile_kernel(const __g
                                       v0 + BN - 1 > info.it.row0 + first_tok};
                     const float unit = biased || (I8 && !Half2Of<T>::is_bf16) ? 1.0f : shape.unit;     // that shaping has left to do
                     const uint32_t my_half = my_s + 64 * half;         // its scores, then its weights
-                    // Weights that are in place, of chunks before c.
+                    // Weights that are in place, of chunks before c. Their stores are waited for: nothing else orders a load from tensor memory
+                    // behind a store to the same columns.
                     auto rescale = [&](int c, float f) {
+                        wait_st();
 #pragma unroll 1
                         for (int x = 0; x < 16 * c; x += 16) {
                             float w[16];
