@@ -395,12 +395,27 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
 #pragma unroll
                         for (int u = 0; u < 2; ++u) edge |= pos_of[u] < 0 || pos_of[u] + 15 > open || (a.window > 0 && pos_of[u] <= info.pos_last - a.window);
 #pragma unroll
-                        for (int u = 0; u < 2; ++u)
+                        for (int u = 0; u < 2; ++u) {
+                            if constexpr (FORM) {                      // the scores, capped
+                                float z[NT * 4];
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) {
+                                    const bool real = !edge || (pos_of[u] >= 0 && pos_of[u] + r8 + 8 * h < info.kv);
+                                    const float k_in = real ? scales[16 * u + 8 * h] * a.score_in : 0.0f;
+#pragma unroll
+                                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                        for (int i = 0; i < 2; ++i) z[n * 4 + 2 * h + i] = sc[u][n][2 * h + i] * (k_in * q_unit[n][i]);
+                                }
+                                if (a.cap2 > 0.0f) tanh_of_few(z);
+#pragma unroll
+                                for (int x = 0; x < NT * 4; ++x) sc[u][x / 4][x % 4] = a.cap2 > 0.0f ? z[x] * a.cap2 : z[x];
+                            }
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {              // keys r8 and r8 + 8
                                 const int kp = pos_of[u] + r8 + 8 * h;
                                 const bool real = !edge || (pos_of[u] >= 0 && kp < info.kv);      // others have codes and scales of any kind
-                                const float k_in = real ? scales[16 * u + 8 * h] * (FORM ? a.score_in : a.scale_log2) : 0.0f;
+                                const float k_in = !FORM && real ? scales[16 * u + 8 * h] * a.scale_log2 : 0.0f;
                                 const float v_scale = real ? scales[TILE + 16 * u + 8 * h] : 0.0f, v = v_scale > 0.0f ? v_scale : kZeroScale, v_log = lg2(v);
                                 v_inv[u][h] = rcp(v);
 #pragma unroll
@@ -409,8 +424,6 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                                     for (int i = 0; i < 2; ++i) {
                                         float& y = sc[u][n][2 * h + i];
                                         if constexpr (FORM) {
-                                            y *= k_in * q_unit[n][i];
-                                            if (a.cap2 > 0.0f) y = capped(y, a.cap2);
                                             if (a.slopes) y -= slope[n][i] * static_cast<float>(abs(qown[n][i] - kp));
                                             y += v_log;
                                         } else y = fmaf(y, k_in * q_unit[n][i], v_log);
@@ -418,6 +431,7 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                                         grow |= y > m[n][i] + Range::grow;
                                     }
                             }
+                        }
                         if (__any_sync(0xffffffffu, grow)) {
                             auto highest = [](float x) {               // of the column's keys
                                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 4));
@@ -516,16 +530,22 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                     const int open = FORM && info.pos0 >= 0 ? max(info.pos0, info.prefix - 1) : info.pos0;       // last position visible to every row
                     const bool edge = pos + 15 > open || (a.window > 0 && pos <= info.pos_last - a.window);
                     bool grow = false;
+                    if constexpr (FORM) {
+                        float z[NT * 4];
+#pragma unroll
+                        for (int x = 0; x < NT * 4; ++x) z[x] = sc[x / 4][x % 4] * a.score_in;
+                        if (a.cap2 > 0.0f) tanh_of_few(z);
+#pragma unroll
+                        for (int x = 0; x < NT * 4; ++x) sc[x / 4][x % 4] = a.cap2 > 0.0f ? z[x] * a.cap2 : z[x];
+                    }
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const int i = j & 1, kp = pos + r8 + (j >> 1) * 8;
-                            sc[n][j] *= FORM ? a.score_in : a.scale_log2;
                             if constexpr (FORM) {
-                                if (a.cap2 > 0.0f) sc[n][j] = capped(sc[n][j], a.cap2);
                                 if (a.slopes) sc[n][j] -= slope[n][i] * static_cast<float>(abs(qown[n][i] - kp));
-                            }
+                            } else sc[n][j] *= a.scale_log2;
                             if (edge && (kp > (FORM ? qend[n][i] : qpos[n][i]) || (a.window > 0 && kp <= qpos[n][i] - a.window))) sc[n][j] = -INFINITY;
                             grow |= sc[n][j] > m[n][i] + Range::grow;
                         }

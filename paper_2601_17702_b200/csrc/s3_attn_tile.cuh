@@ -320,7 +320,7 @@ __device__ __forceinline__ void tanh_of(float (&s)[32])
 }
 
 // 32 scores, from column 32 c of the tile: times the keys' scales, capped (in units of the cap), less what the distance costs; f16 over 8-bit
-// pages: plus the logarithm of the value's scale. The unit is left to the weights where neither of the last two is done. Where all 32 rows' scores here are within the cap, tanh is a polynomial: per key tile and row, two special
+// pages: plus the logarithm of the value's scale. The unit is left to the weights where neither of the last two is done. Where all 32 rows' scores here are within the cap, tanh is a polynomial alone: per key tile and row, two special
 // functions more for each score would take twice the 1024 clocks that the weights' exponentials take.
 template <class T, bool I8>
 __device__ __forceinline__ void shape_scores(float (&s)[32], int c, const Shape& f, const TileScales<T>& by_key)
@@ -341,12 +341,12 @@ __device__ __forceinline__ void shape_scores(float (&s)[32], int c, const Shape&
         float most = 0.0f;
 #pragma unroll
         for (int x = 0; x < 32; x += 2) most = max3(most, fabsf(s[x]), fabsf(s[x + 1]));
-        // (neither if one is NaN)
+        // (neither if one is NaN, which either form passes on)
         if (__all_sync(0xffffffffu, most <= 0.5f)) tanh_of<5>(s);
         else if (__all_sync(0xffffffffu, most <= 1.0f)) tanh_of<7>(s);
         else {
 #pragma unroll
-            for (int x = 0; x < 32; ++x) s[x] = capped(s[x], 1.0f);
+            for (int x = 0; x < 32; ++x) s[x] = tanh_any(s[x]);
         }
     }
     if (f.biased) {

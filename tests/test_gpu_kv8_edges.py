@@ -73,3 +73,36 @@ def test_scores_that_rise_within_64_keys(make, dtype, rows, form):
     d.fine()
     # a score is off by 2^-21 of 128 * 1.35 * 1.2 scale < 20, a cap of 100 by another 100 * 2^-21, a slope's term (up to 9) by 9 * 2^-22
     close(s, got, lambda s: R8.scored(s, **host))
+
+
+# ---------------------------------------------------------------------------------------------- caps far from the scores
+@pytest.mark.parametrize("make", [R.Setup, R8.Setup8])
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("cap", [3.0, 1e4, 1e6, 1e9, 1e20])
+@pytest.mark.parametrize("rows", [1, 3, 80])
+def test_caps_that_change_next_to_nothing(make, dtype, cap, rows):
+    """Under a cap far above the scores tanh(z) is next to z: what is lost may count against the score, not against the cap. Some scores of the
+    last sequence are beyond the cap of 3, so that a warp meets both forms."""
+    s = make([(rows, 600), (rows, 130)], 8, 2, 128, 32, dtype, seed=rows)
+    s.q[: s.cu[1]] *= 0.2 if cap == 3.0 else 2.0
+    d = Device(s)
+    got = S.s3_paged_attention_scored(d.cache, d.batch, d.q, d.ws, cap=cap, want_lse=True)
+    d.fine()
+    close(s, got, lambda s: R8.scored(s, cap=cap))            # a relative error of tanh of 2^-21 is 2^-21 of scores of up to 30: 1.4e-5
+
+
+@pytest.mark.parametrize("make", [R.Setup, R8.Setup8])
+def test_few_rows_and_many_agree_under_a_large_cap(make):
+    """The last row of a chunk and the same row as a step of its own."""
+    s = make([(80, 700)], 8, 2, 128, 64, seed=4)
+    one = make([(1, 700)], 8, 2, 128, 64, seed=4)
+    d, e = Device(s), Device(one)
+    for cap in (1e4, 1e7):
+        out, lse = S.s3_paged_attention_scored(d.cache, d.batch, d.q, d.ws, cap=cap, want_lse=True)
+        e = Device(one)
+        e.cache = d.cache
+        batch = S.KvBatch(torch.tensor([0, 1], dtype=torch.int32, device="cuda"), d.batch.kv_len, d.batch.pages, 1, 1, 700)
+        got, l1 = S.s3_paged_attention_scored(d.cache, batch, d.q[-1:].contiguous(), e.ws, cap=cap, want_lse=True)
+        # each is within eps (|out| + mean |v|) of the definition, |out| and the mean below 1.5 here
+        assert ((got[0] - out[-1]).abs().float() <= 2 * EPS[s.dtype] * 3.0).all()
+        assert ((l1[0] - lse[-1]).abs() <= 4e-5 * lse[-1].abs().clamp(min=1)).all()
