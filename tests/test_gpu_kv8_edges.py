@@ -106,3 +106,30 @@ def test_few_rows_and_many_agree_under_a_large_cap(make):
         # each is within eps (|out| + mean |v|) of the definition, |out| and the mean below 1.5 here
         assert ((got[0] - out[-1]).abs().float() <= 2 * EPS[s.dtype] * 3.0).all()
         assert ((l1[0] - lse[-1]).abs() <= 4e-5 * lse[-1].abs().clamp(min=1)).all()
+
+
+# ---------------------------------------------------------------------------------------------- what must not matter
+@pytest.mark.parametrize("make", [R.Setup, R8.Setup8])
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("H,K", [(14, 2), (9, 3), (8, 2)])
+@pytest.mark.parametrize("form", [dict(cap=1e3), dict(cap=30.0, window=70), dict(cap=1e3, slopes=True)])
+def test_what_does_not_count_changes_no_bit(make, dtype, H, K, form):
+    """Page tails of anything against page tails of zeros, and shared memory that another call has left: 7 heads to a group leave two of a tile's
+    128 rows unwritten, a group of 3 as well."""
+    results = []
+    lens = [(40, 333), (90, 90), (1, 7)]
+    for outside in (0.0, float("nan"), float("inf")):
+        s = make(lens, H, K, 128, 64, dtype, seed=3, outside=outside)
+        if outside != 0.0:                                   # many rows of large numbers first, in tiles of their own
+            loud = R.Setup([(300, 400)], 8, 2, 128, 64, dtype, seed=1)
+            loud.q = loud.q * 100
+            e = Device(loud)
+            S.s3_paged_attention(e.cache, e.batch, e.q, e.ws)
+        d = Device(s)
+        dev = dict(form)
+        if form.get("slopes"):
+            dev["slopes"] = torch.linspace(-0.01, 0.1, H, device="cuda")
+        results.append(S.s3_paged_attention_scored(d.cache, d.batch, d.q, d.ws, want_lse=True, **dev))
+        d.fine()
+    for out, lse in results[1:]:
+        assert torch.equal(out, results[0][0]) and torch.equal(lse, results[0][1])
