@@ -51,9 +51,17 @@ constexpr int TMEM_COLS = 512;
 
 // Forms of the score: none; a prefix, which only changes what is masked; shaped (capped or biased, with a prefix or not); capped only, by
 // so little that 2^cap and sums of it are numbers of the rows' type: then the reference is 0 for good and a row's two threads need not meet
-// (2048 tokens over 16384 keys 757 us with references, 632 without, 702 as a choice at run time within one kernel).
+// (as a choice at run time within one kernel half of what that saves is lost).
+//
+// Without a reference weights lie within 2^-80 and 2^80, so that values of 2^48 and above may leave fp32 (8-bit pages: a weight times a value's scale
+// leaves bf16), and where all of a row's scores are low, small values vanish. Neither happens with numbers of ordinary size, and both
+// show in the results: a block that finds one that is not finite, or a sum of weights below kLeastSum, marks itself, and a second launch of the
+// same grid makes its results again with references; the other blocks leave at once (2 to 9 us a call; with references throughout 32 tokens
+// over 300 keys take 18.8 us against 17.9, 512 over 4096 75 against 68, 2048 over 16384 759 against 650). At a sum of kLeastSum or more, what products below
+// fp32's normal numbers lose is less than 2^-102 a key.
 enum { FORM_NONE = 0, FORM_PREFIX = 1, FORM_SHAPED = 2, FORM_BOUNDED = 3 };
-constexpr float kBoundedCap = 80.0f;       // base 2: a sum of 2^30 weights, times values of 2^17, stays in fp32 and bf16
+constexpr float kBoundedCap = 80.0f;       // base 2
+constexpr float kLeastSum = 5.9604645e-8f; // 2^-24
 
 // Four role warps and a softmax thread per query row, or two where scores are shaped; 8-bit pages: warps 2 and 3 and four more widen tiles.
 __host__ __device__ constexpr int softmax_warps(int form) { return form >= FORM_SHAPED ? 16 : 8; }
@@ -475,10 +483,16 @@ __global__ void __launch_bounds__(threads_of(I8, FORM), 1) tile_kernel(const __g
     SegInfo* infos = reinterpret_cast<SegInfo*>(scales_full + 4);
     uint32_t& tmem_slot = *reinterpret_cast<uint32_t*>(infos + 2);
     volatile uint32_t* abort_flag = &tmem_slot + 1;
-    static_assert((2 * SLOTS + 29 + 2 * L::RAW) * 8 + 2 * sizeof(SegInfo) + 8 <= 640, "barriers and descriptions fit");
+    volatile uint32_t* redo_flag = &tmem_slot + 2;
+    static_assert((2 * SLOTS + 29 + 2 * L::RAW) * 8 + 2 * sizeof(SegInfo) + 12 <= 640, "barriers and descriptions fit");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     cudaTriggerProgrammaticLaunchCompletion();       // the join's blocks may take their places; they wait for this grid's end
+    if constexpr (FORM == FORM_SHAPED)
+        if (a.redo) {                                // the second launch: only what the first has marked
+            cudaGridDependencySynchronize();
+            if (a.redo[blockIdx.x] == 0) return;
+        }
     if (threadIdx.x == 0) {
         for (int i = 0; i < SLOTS; ++i) { mbar_init(&full_bar[i], I8 ? WIDEN : 1); mbar_init(&empty_bar[i], 1); }
         for (int i = 0; i < L::RAW; ++i) { mbar_init(&raw_full[i], 1); mbar_init(&raw_empty[i], WIDEN); }
@@ -497,6 +511,7 @@ __global__ void __launch_bounds__(threads_of(I8, FORM), 1) tile_kernel(const __g
         mbar_init(&meet_bar, 4);
         mbar_init(&met_bar, SHAPED ? 8 : 4);
         *abort_flag = 0;
+        *redo_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -1201,6 +1216,7 @@ __global__ void __launch_bounds__(threads_of(I8, FORM), 1) tile_kernel(const __g
                 }
                 // with two threads per row and head_dim 128 each writes half of it
                 const int c_lo = SHAPED && half == 1 ? (D == 128 ? 64 : D) : 0, c_hi = SHAPED && half == 0 && D == 128 ? 64 : D;
+                float largest = 0.0f;                                  // magnitude of this thread's results, NaN if one is
                 // a store's lane writes piece lane % 8 of the lines of rows x + 8 (lane / 8)
                 auto scaled = [&](int c, float (&o)[32]) {             // 32 results of this lane's row
                     tm_ld32(my_o + c, o);
@@ -1214,6 +1230,9 @@ __global__ void __launch_bounds__(threads_of(I8, FORM), 1) tile_kernel(const __g
 #pragma unroll
                         for (int x = 0; x < 32; ++x) o[x] = empty ? 0.0f : fmaf(z[x], f_other, o[x]);
                     }
+                    if constexpr (bounded)
+#pragma unroll
+                        for (int x = 0; x < 32; x += 2) largest = max3(largest, fabsf(o[x]), fabsf(o[x + 1]));
                 };
                 const uint32_t alive = __ballot_sync(0xffffffffu, live);
                 const int my_piece = lane & 7, my_row = lane & 24;
@@ -1254,6 +1273,7 @@ __global__ void __launch_bounds__(threads_of(I8, FORM), 1) tile_kernel(const __g
                         }
                     }
                 }
+                if (bounded && live && !(largest < INFINITY && (empty || l >= kLeastSum))) *redo_flag = 1;
                 tc_fence_before();
                 __syncwarp();
                 if (!PAIR && lane == 0) mbar_arrive(&met_bar);
@@ -1267,6 +1287,7 @@ __global__ void __launch_bounds__(threads_of(I8, FORM), 1) tile_kernel(const __g
     if constexpr (I8)
         if (warp == 2 || warp == 3 || warp >= 4 + softmax_warps(FORM)) widen(warp < 4 ? warp - 2 : warp - 2 - softmax_warps(FORM));
     __syncthreads();
+    if (FORM == FORM_BOUNDED && threadIdx.x == 0) a.redo[blockIdx.x] = *redo_flag != 0;
     if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLS) : "memory");
@@ -1310,10 +1331,14 @@ s3_status launch_typed(const KvCacheState& c, const AttnArgs& a, cudaStream_t st
 
 // The form of a call that has one.
 template <bool I8>
-s3_status launch_form(const KvCacheState& c, const AttnArgs& a, cudaStream_t stream)
+s3_status launch_form(const KvCacheState& c, const AttnArgs& args, cudaStream_t stream)
 {
+    AttnArgs a = args;
     if (!(a.cap2 > 0.0f) && !a.slopes) return launch_typed<I8, FORM_PREFIX>(c, a, stream);
-    if (c.d.dtype == S3_BF16 && !a.slopes && a.cap2 <= kBoundedCap) return launch_typed<I8, FORM_BOUNDED>(c, a, stream);
+    if (c.d.dtype == S3_BF16 && !a.slopes && a.cap2 <= kBoundedCap && a.redo) {
+        const s3_status st = launch_typed<I8, FORM_BOUNDED>(c, a, stream);
+        if (st != S3_OK) return st;
+    } else a.redo = nullptr;                                           // all of it
     return launch_typed<I8, FORM_SHAPED>(c, a, stream);
 }
 

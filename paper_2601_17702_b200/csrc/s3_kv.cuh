@@ -174,6 +174,7 @@ struct AttnArgs {
     int32_t* cuts;              // [grid][8]: the unit that the cut behind a block's share divides first, see Cut
     int32_t grid, share_min, whole_rounds, rows_cap, tok_per_item, n_items, one_item_per_seq;
     uint32_t* status;
+    uint8_t* redo;              // [grid] or null: blocks whose results have to be made again, see FORM_BOUNDED in s3_attn_tile.cuh
 };
 
 struct AttnItem {

@@ -339,6 +339,8 @@ s3_status attention(const s3_kv_cache* cache, const s3_kv_batch* batch, const vo
     a.n_items = p.n_items;
     a.one_item_per_seq = p.one_item_per_seq;
     a.status = static_cast<uint32_t*>(d_ws);
+    // a byte per block of the tile kernel, between the status block and the pieces
+    a.redo = ws_bytes >= 256 && p.grid <= 256 - S3_WS_HEADER_BYTES ? static_cast<uint8_t*>(d_ws) + S3_WS_HEADER_BYTES : nullptr;
 
     a.grid = p.grid;
     a.share_min = p.share_min;

@@ -133,3 +133,85 @@ def test_what_does_not_count_changes_no_bit(make, dtype, H, K, form):
         d.fine()
     for out, lse in results[1:]:
         assert torch.equal(out, results[0][0]) and torch.equal(lse, results[0][1])
+
+
+# ---------------------------------------------------------------------------------------------- numbers at the ends of their types
+def along(s, rows, amount):
+    """Queries and keys along one direction, so that the products are large: score sign(keys of the block) * amount (before a cap)."""
+    key = torch.randn(s.D, generator=s.g)
+    key *= (s.D / key.square().sum()).sqrt()
+    s.q = (key + 0.05 * torch.randn(s.q.shape, generator=s.g)).to(s.dtype)
+    for i, (_, kv) in enumerate(s.lens):
+        for j in range(-(-kv // s.P)):
+            p, n = int(s.pages[i, j]), min(s.P, kv - s.P * j)
+            k = (key * amount(j) / s.D ** 0.5 + 0.1 * torch.randn((s.K, n, s.D), generator=s.g)).to(s.dtype)
+            if hasattr(s, "k8"):
+                s.k8[p, :, :n], s.k_scale[p, :, :n] = R8.held8(k)
+            else:
+                s.k_cache[p, :, :n] = k
+
+
+def values_times(s, factor):
+    for p in range(s.n_pages):
+        f = factor(p)
+        if hasattr(s, "v8"):
+            s.v_scale[p] *= f
+        else:
+            s.v_cache[p] *= f
+
+
+@pytest.mark.parametrize("make", [R.Setup, R8.Setup8])
+@pytest.mark.parametrize("rows,lens", [(1, [(1, 300)]), (70, [(70, 300), (70, 150)]), (300, [(300, 2000)])])
+@pytest.mark.parametrize("size", [2.0 ** 56, 2.0 ** -56, 1.0])
+@pytest.mark.parametrize("sign", [1, -1, 0])
+@pytest.mark.parametrize("cap", [30.0, 50.0])
+def test_values_of_any_size_at_either_end_of_the_cap(make, rows, lens, size, sign, cap):
+    """All scores next to the cap, all next to its negative, or some blocks here and some there; values of 2^56 (codes times scales of up to
+    2^58), of 1, and as small; some pages in between, so that not every thread block meets them."""
+    s = make(lens, 8, 2, 128, 64, seed=rows)
+    along(s, rows, lambda j: 200.0 * (sign if sign else (1 if j % 3 else -1)))
+    values_times(s, lambda p: size)
+    d = Device(s)
+    got = S.s3_paged_attention_scored(d.cache, d.batch, d.q, d.ws, scale=128 ** -0.5, cap=cap, want_lse=True)
+    d.fine()
+    # scores of 200 to 300 from products of 128 terms whose magnitudes add up to as much: off by 300 * 2^-21, and less behind the cap
+    close(s, got, lambda s: R8.scored(s, scale=128 ** -0.5, cap=cap), slack=3e-4)
+
+
+@pytest.mark.parametrize("make", [R.Setup, R8.Setup8])
+def test_marked_blocks_leave_the_others_alone(make):
+    """Large values in one sequence of several: its rows are right, and the others have the bits that they have without it. A replayed graph whose
+    values become ordinary, and large again, follows."""
+    lens = [(70, 400), (70, 500), (40, 300)]
+    s = make(lens, 8, 2, 128, 64, seed=5)
+    along(s, 70, lambda j: 100.0 if j % 2 else 20.0)
+    d = Device(s)
+    run = lambda: S.s3_paged_attention_scored(d.cache, d.batch, d.q, d.ws, cap=50.0, want_lse=True)
+    plain = [t.clone() for t in run()]
+    big = [int(p) for p in s.pages[1, :8]]
+    target, host = (d.vs, s.v_scale) if make is R8.Setup8 else (d.v, s.v_cache)
+    keep = target.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            got = run()
+    side.synchronize()
+    for large in (True, False, True):
+        target.copy_(keep)
+        if large:
+            target[big] *= 2.0 ** 57
+        with torch.cuda.stream(side):
+            side.wait_stream(torch.cuda.default_stream())
+            g.replay()
+        side.synchronize()
+        for a, b in zip(got, plain):
+            assert torch.equal(a[:70], b[:70]) and torch.equal(a[140:], b[140:])
+            if not large:
+                assert torch.equal(a, b)
+        assert torch.isfinite(got[0]).all()
+    host[big] *= 2.0 ** 57
+    close(s, got, lambda s: R8.scored(s, cap=50.0), slack=3e-4)
+    d.fine()
