@@ -566,7 +566,8 @@ s3_status s3_fuse_index_sets(const int32_t* d_centers, int Q, int n_centers, int
  * What a call never uses, whatever it holds (NaN too): positions >= kv_len, pages and blocks that are not listed, table
  * entries past the length, and for attention with a window pages (and their table entries) that lie before the window of
  * every new row of the sequence. Keys that a row may not see do not enter its result; VALUES at positions < kv_len of a block that
- * the call reads must be finite (a zero weight times an infinity is a NaN).
+ * the call reads must be finite (a zero weight times an infinity is a NaN), and their magnitudes add up to less than 2^112 in each dimension (they
+ * are summed in fp32 with weights of up to 2^15).
  *
  * All row pitches are in elements, multiples of 8, heads contiguous within a row (a slice of a fused projection will do);
  * pointers to rows, pages, summaries, rotation tables and the workspace 16-byte aligned, all others 4-byte (a call refuses what is not). One

@@ -380,10 +380,10 @@ __device__ __forceinline__ void shape_scores(float (&s)[32], int c, const Shape&
     }
 }
 
-// Sum of 32 weights up to which the reference stays: bf16 has the exponents of fp32, and any reference below a score will do; in f16 no weight may
-// exceed 65504.
+// Sum of 32 weights up to which the reference stays: in f16 no weight may exceed 65504; bf16 has the exponents of fp32, but weights times
+// values are summed in fp32, so it is what unshaped scores may reach (2^32 left no room for values of 2^90).
 template <class T>
-constexpr float kMostSum = Half2Of<T>::is_bf16 ? 4294967296.0f : 32768.0f;
+constexpr float kMostSum = Half2Of<T>::is_bf16 ? 16384.0f : 32768.0f;
 
 // 2^x of a whole number x <= 0, exactly; 0 below the normal range. References of shaped scores are whole numbers, so that weights which
 // have been rounded already can follow one without another rounding.

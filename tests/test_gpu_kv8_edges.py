@@ -215,3 +215,22 @@ def test_marked_blocks_leave_the_others_alone(make):
     host[big] *= 2.0 ** 57
     close(s, got, lambda s: R8.scored(s, cap=50.0), slack=3e-4)
     d.fine()
+
+
+@pytest.mark.parametrize("rows", [1, 100, 300])
+@pytest.mark.parametrize("form", [dict(), dict(slopes=True), dict(cap=300.0), dict(cap=50.0)])
+@pytest.mark.parametrize("rise", [17.0, 20.0])
+def test_large_values_under_scores_that_rise(rows, form, rise):
+    """bf16 values of 2^101 (their magnitudes add up to 2^111) over scores that are 17 or 20 higher (base 2: 25, 29) from the third block on than before: the
+    weights stay small enough that sums in fp32 hold them."""
+    s = R.Setup([(rows, 900), (rows, 500)], 8, 2, 128, 64, seed=rows)
+    along(s, rows, lambda j: 10.0 + rise if j >= 2 else 10.0)
+    values_times(s, lambda p: 2.0 ** 101)
+    host = dict(form)
+    if form.get("slopes"):
+        host["slopes"] = torch.linspace(0.0, 0.001, 8)
+    dev = {k: v.cuda() if torch.is_tensor(v) else v for k, v in host.items()}
+    d = Device(s)
+    got = S.s3_paged_attention_scored(d.cache, d.batch, d.q, d.ws, scale=128 ** -0.5, want_lse=True, **dev)
+    d.fine()
+    close(s, got, lambda s: R8.scored(s, scale=128 ** -0.5, **host))
