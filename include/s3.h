@@ -602,7 +602,9 @@ s3_status s3_kv_cache_destroy(s3_kv_cache* cache);
  *   scale = max_d |x[d]| / 127,   code[d] = rint(127 x[d] / max_d |x[d]|)     (a row whose largest magnitude is below 2^-60: zeros)
  * and stands for code * scale. A NaN counts as 0, a magnitude beyond 2^60 (S3_F16: 65504) as that. Keys are taken as the append computes
  * them, in 64 bits and not rounded to the rows' type before; ties go to the even code. Every call below takes such a cache; summaries are of
- * the keys that the codes stand for. Where a call reads positions < kv_len of a block, their scales must be finite. */
+ * the keys that the codes stand for. Where a call reads positions < kv_len of a block, their scales must be finite; they may have
+ * either sign. A caller who writes value scales keeps them at 0 or within [2^-67, 2^53] in magnitude (S3_F16: [2^-31, 2^9], what an append writes);
+ * attention may take a smaller one for 0. */
 s3_status s3_kv_cache_create_i8(s3_kv_cache** out, const s3_kv_cache_desc* desc, float* d_k_scale, float* d_v_scale);
 /* Scratch that suffices for every call over this batch (or one with smaller bounds) with n_heads query heads. */
 size_t s3_kv_workspace_bytes(const s3_kv_cache* cache, const s3_kv_batch* batch, int n_heads);

@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                         const float* scales = reinterpret_cast<const float*>(ring + L::SCALES) + st * 2 * TILE + warp * 32 + r8;
                         // S^T = K Q^T: lane (r8, quad) holds rows r8 and r8 + 8 of K, dimensions D / 4 quad and on, in the order in which they lie
                         constexpr int W = D / 64;                      // 16-byte pieces per row and lane
-                        float sc[2][NT][4], v_inv[2][2];               // exponents of the weights, the values' scales in them; their inverses
+                        float sc[2][NT][4], v_inv[2][2], v_sign[2][2]; // exponents of the weights, the values' scales in them; their inverses; 1, -1 or 0
                         bool grow = false;
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
@@ -416,7 +416,10 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                                 const int kp = pos_of[u] + r8 + 8 * h;
                                 const bool real = !edge || (pos_of[u] >= 0 && kp < info.kv);      // others have codes and scales of any kind
                                 const float k_in = !FORM && real ? scales[16 * u + 8 * h] * a.scale_log2 : 0.0f;
-                                const float v_scale = real ? scales[TILE + 16 * u + 8 * h] : 0.0f, v = v_scale > 0.0f ? v_scale : kZeroScale, v_log = lg2(v);
+                                const float v_scale = real ? scales[TILE + 16 * u + 8 * h] : 0.0f;
+                                const bool some = fabsf(v_scale) >= kLeastScale<T>;
+                                const float v = some ? fabsf(v_scale) : kZeroScale, v_log = lg2(v);
+                                v_sign[u][h] = some ? copysignf(1.0f, v_scale) : 0.0f;
                                 v_inv[u][h] = rcp(v);
 #pragma unroll
                                 for (int n = 0; n < NT; ++n)
@@ -467,6 +470,7 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                                 for (int j = 0; j < 4; ++j) {
                                     y[j] = ex2(sc[u][n][j] - (m[n][j & 1] == -INFINITY ? 0.0f : m[n][j & 1]));
                                     l[n][j & 1] = fmaf(y[j], v_inv[u][j >> 1], l[n][j & 1]);
+                                    y[j] *= v_sign[u][j >> 1];
                                 }
                                 p[n][0] = transpose8(Half2Of<__half>::pack(y[0], y[1]));
                                 p[n][1] = transpose8(Half2Of<__half>::pack(y[2], y[3]));

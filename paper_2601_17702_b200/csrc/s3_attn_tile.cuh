@@ -86,6 +86,11 @@ struct TileWhere {
     int unclean, unused[7];
 };
 
+// 8-bit pages, f16: keys of a tile whose values count as 0, and whose scales are negative.
+struct TileOdd {
+    uint32_t off[BN / 32], neg[BN / 32];
+};
+
 // 8-bit pages: what the softmax needs of a key tile's scales, made by the converting warps.
 template <class T>
 struct TileScales {
@@ -113,7 +118,8 @@ struct Layout {
     static constexpr int SHARE = MEET + (FORM >= FORM_SHAPED && PAIR ? 0 : 1024);
     static constexpr int WHERE = SHARE + (FORM >= FORM_SHAPED ? 2 * 2 * 128 * 4 + 64 : 0);        // positions of the key tiles in flight, for lists
     static constexpr int BARS = WHERE + (FORM ? 0 : 8 * static_cast<int>(sizeof(TileWhere)));         // forms come without lists
-    static constexpr int TOTAL = BARS + 640;
+    static constexpr int ODD = BARS + 640;                                                            // entries as of SCALES
+    static constexpr int TOTAL = ODD + (I8 && !Half2Of<T>::is_bf16 ? 4 * static_cast<int>(sizeof(TileOdd)) : 0);
     static_assert(TOTAL <= 227 * 1024, "one thread block per SM");
 };
 
@@ -480,6 +486,7 @@ __global__ void __launch_bounds__(threads_of(I8, FORM), 1) tile_kernel(const __g
     // come free for that one: at least the second load after this tile's values has then been consumed (no more than five slots), hence
     // this tile's weights, which are made after the last read of its scales.
     TileScales<T>* scales = reinterpret_cast<TileScales<T>*>(smem + L::SCALES);
+    TileOdd* odd = reinterpret_cast<TileOdd*>(smem + L::ODD);
     SegInfo* infos = reinterpret_cast<SegInfo*>(scales_full + 4);
     uint32_t& tmem_slot = *reinterpret_cast<uint32_t*>(infos + 2);
     volatile uint32_t* abort_flag = &tmem_slot + 1;
@@ -511,7 +518,7 @@ __global__ void __launch_bounds__(threads_of(I8, FORM), 1) tile_kernel(const __g
         mbar_init(&meet_bar, 4);
         mbar_init(&met_bar, SHAPED ? 8 : 4);
         *abort_flag = 0;
-        *redo_flag = 0;
+        if constexpr (FORM == FORM_BOUNDED) *redo_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -584,9 +591,15 @@ __global__ void __launch_bounds__(threads_of(I8, FORM), 1) tile_kernel(const __g
                     const float v = real ? in[BN + key] : 0.0f;
                     if constexpr (Half2Of<T>::is_bf16) out.v[key] = v;
                     else {
-                        const float some = v > 0.0f ? v : kZeroScale;
-                        out.v[key] = 1.0f / some;
-                        out.v_log[key] = lg2(some);
+                        const bool some = fabsf(v) >= kLeastScale<T>;
+                        const float size = some ? fabsf(v) : kZeroScale;
+                        out.v[key] = 1.0f / size;
+                        out.v_log[key] = lg2(size);
+                        const uint32_t off = __ballot_sync(0xffffffffu, real && !some), neg = __ballot_sync(0xffffffffu, v < 0.0f);
+                        if (lane == 0) {
+                            odd[(tile + j) & 3].off[me] = off;
+                            odd[(tile + j) & 3].neg[me] = neg;
+                        }
                     }
                 }
                 __syncwarp();
@@ -840,6 +853,28 @@ __global__ void __launch_bounds__(threads_of(I8, FORM), 1) tile_kernel(const __g
                             }
                             fence_async_smem();
                             __syncwarp();
+                        }
+                        if constexpr (I8 && !Half2Of<T>::is_bf16) {
+                            // what a logarithm cannot say of a value's scale, that it is 0 and its sign, goes into the codes, row by row (in the warps that
+                            // widen them, with two bits per row, it cost 80 us of 1412 for 2048 tokens over 32768 keys without any such row, here 43)
+                            const TileOdd& of = odd[tile & 3];
+                            const uint32_t off = of.off[lane & 3], neg = of.neg[lane & 3];
+                            if (__any_sync(0xffffffffu, (off | neg) != 0)) {
+                                unsigned char* tile_v = ring + sv * L::TILE_BYTES;
+                                for (int w = 0; w < BN / 32; ++w) {
+                                    const uint32_t gone = of.off[w], turned = of.neg[w];
+                                    for (uint32_t rows = gone | turned; rows; rows &= rows - 1) {
+                                        const int bit = __ffs(rows) - 1, row = 32 * w + bit;
+                                        const uint32_t keep = gone >> bit & 1u ? 0u : 0xffffffffu, flip = turned >> bit & 1u ? 0x80008000u : 0u;
+                                        if (lane < D / 8) {            // a row's 16-byte pieces, in whatever order
+                                            uint4& y = *reinterpret_cast<uint4*>(tile_v + (lane >> 3) * BN * 128 + row * 128 + (lane & 7) * 16);
+                                            y = make_uint4((y.x & keep) ^ flip, (y.y & keep) ^ flip, (y.z & keep) ^ flip, (y.w & keep) ^ flip);
+                                        }
+                                    }
+                                }
+                                fence_async_smem();
+                                __syncwarp();
+                            }
                         }
                         const bool more = j + AHEAD < n_tiles;
                         const uint32_t sk = used % SLOTS;

@@ -234,3 +234,44 @@ def test_large_values_under_scores_that_rise(rows, form, rise):
     got = S.s3_paged_attention_scored(d.cache, d.batch, d.q, d.ws, scale=128 ** -0.5, want_lse=True, **dev)
     d.fine()
     close(s, got, lambda s: R8.scored(s, scale=128 ** -0.5, **host))
+
+
+# ---------------------------------------------------------------------------------------------- scales that a caller wrote
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("lens", [[(1, 300), (1, 17)], [(70, 300), (40, 200)], [(300, 500)]])
+@pytest.mark.parametrize("form", [None, dict(cap=20.0), dict(slopes=True)])
+@pytest.mark.parametrize("D,P", [(128, 16), (64, 64)])
+def test_rows_switched_off_and_turned_over(dtype, lens, form, D, P):
+    """A value scale of 0 over codes that are not, negative scales of keys and values, scales below any that an append writes: a row counts for
+    code * scale whatever wrote it."""
+    s = R8.Setup8(lens, 8, 2, D, P, dtype, seed=len(lens))
+    x = torch.randint(0, 8, s.v_scale.shape, generator=s.g)
+    s.v_scale[x == 0] = 0.0
+    s.v_scale[x == 1] *= -1.0
+    s.v_scale[x == 2] = 1e-40
+    s.v_scale[x == 3] = -(2.0 ** -75)
+    s.k_scale[torch.randint(0, 4, x.shape, generator=s.g) == 0] *= -1.0
+    d = Device(s)
+    if form is None:
+        got, ref = S.s3_paged_attention(d.cache, d.batch, d.q, d.ws, want_lse=True), lambda s: R.attention(s)
+    else:
+        host = dict(form)
+        if form.get("slopes"):
+            host["slopes"] = torch.linspace(0.0, 0.1, 8)
+        dev = {k: v.cuda() if torch.is_tensor(v) else v for k, v in host.items()}
+        got, ref = S.s3_paged_attention_scored(d.cache, d.batch, d.q, d.ws, want_lse=True, **dev), lambda s: R8.scored(s, **host)
+    d.fine()
+    close(s, got, ref)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("per_token,q", [(True, 1), (True, 90), (False, 90)])
+def test_switched_off_rows_in_lists(dtype, per_token, q):
+    s = R8.Setup8([(q, 700)], 8, 2, 128, 64, dtype, seed=q)
+    s.v_scale[torch.randint(0, 3, s.v_scale.shape, generator=s.g) == 0] = 0.0
+    s.v_scale[torch.randint(0, 3, s.v_scale.shape, generator=s.g) == 0] *= -1.0
+    lists = torch.stack([torch.stack([torch.randperm(11, generator=s.g)[:6] for _ in range(2)]) for _ in range(q if per_token else 1)]).to(torch.int32)
+    d = Device(s)
+    got = S.s3_block_attention(d.cache, d.batch, d.q, lists.cuda(), d.ws, per_token=per_token, want_lse=True)
+    d.fine()
+    close(s, got, lambda s: R.attention(s, blocks=lists, per_token=per_token))
