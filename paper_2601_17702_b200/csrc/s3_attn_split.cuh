@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                         const float* scales = reinterpret_cast<const float*>(ring + L::SCALES) + st * 2 * TILE + warp * 32 + r8;
                         // S^T = K Q^T: lane (r8, quad) holds rows r8 and r8 + 8 of K, dimensions D / 4 quad and on, in the order in which they lie
                         constexpr int W = D / 64;                      // 16-byte pieces per row and lane
-                        float sc[2][NT][4], v_inv[2][2], v_sign[2][2]; // exponents of the weights, the values' scales in them; their inverses; 1, -1 or 0
+                        float sc[2][NT][4], v_log[2][2], v_sign[2][2]; // exponents of the weights, the values' scales in them; their logarithms; 1, -1 or 0
                         bool grow = false;
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
@@ -418,9 +418,8 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                                 const float k_in = !FORM && real ? scales[16 * u + 8 * h] * a.scale_log2 : 0.0f;
                                 const float v_scale = real ? scales[TILE + 16 * u + 8 * h] : 0.0f;
                                 const bool some = fabsf(v_scale) >= kLeastScale<T>;
-                                const float v = some ? fabsf(v_scale) : kZeroScale, v_log = lg2(v);
+                                v_log[u][h] = lg2(some ? fabsf(v_scale) : kLeastScale<T>);
                                 v_sign[u][h] = some ? copysignf(1.0f, v_scale) : 0.0f;
-                                v_inv[u][h] = rcp(v);
 #pragma unroll
                                 for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -428,8 +427,8 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                                         float& y = sc[u][n][2 * h + i];
                                         if constexpr (FORM) {
                                             if (a.slopes) y -= slope[n][i] * static_cast<float>(abs(qown[n][i] - kp));
-                                            y += v_log;
-                                        } else y = fmaf(y, k_in * q_unit[n][i], v_log);
+                                            y += v_log[u][h];
+                                        } else y = fmaf(y, k_in * q_unit[n][i], v_log[u][h]);
                                         if (edge && (!real || kp > (FORM ? qend[n][i] : qpos[n][i]) || (a.window > 0 && kp <= qpos[n][i] - a.window))) y = -INFINITY;
                                         grow |= y > m[n][i] + Range::grow;
                                     }
@@ -447,9 +446,11 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
 #pragma unroll
                                 for (int i = 0; i < 2; ++i) {
                                     const float top = highest(fmaxf(fmaxf(fmaxf(sc[0][n][i], sc[0][n][2 + i]), fmaxf(sc[1][n][i], sc[1][n][2 + i])) - Range::lift, m[n][i]));
-                                    f[i] = m[n][i] == -INFINITY ? 0.0f : ex2(m[n][i] - top);
+                                    // in two steps: the reference follows the values' scales, and the sum of weights has to outlast them
+                                    const float half = m[n][i] == -INFINITY ? 0.0f : ex2(0.5f * (m[n][i] - top));
+                                    f[i] = half * half;
                                     m[n][i] = top;
-                                    l[n][i] *= f[i];
+                                    l[n][i] = l[n][i] * half * half;
                                 }
 #pragma unroll
                                 for (int k = 0; k < D / 16; ++k) {
@@ -468,9 +469,10 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                                 float y[4];
 #pragma unroll
                                 for (int j = 0; j < 4; ++j) {
-                                    y[j] = ex2(sc[u][n][j] - (m[n][j & 1] == -INFINITY ? 0.0f : m[n][j & 1]));
-                                    l[n][j & 1] = fmaf(y[j], v_inv[u][j >> 1], l[n][j & 1]);
-                                    y[j] *= v_sign[u][j >> 1];
+                                    const float e = sc[u][n][j] - (m[n][j & 1] == -INFINITY ? 0.0f : m[n][j & 1]);
+                                    // the weight without the scale by an exponential of its own: with it, it may be below fp32's numbers
+                                    l[n][j & 1] += ex2(e - v_log[u][j >> 1]);
+                                    y[j] = ex2(e) * v_sign[u][j >> 1];
                                 }
                                 p[n][0] = transpose8(Half2Of<__half>::pack(y[0], y[1]));
                                 p[n][1] = transpose8(Half2Of<__half>::pack(y[2], y[3]));
@@ -647,10 +649,18 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             const float m2 = red_m[x][n * 8 + quad * 2 + i], top = fmaxf(m[n][i], m2), ref = top == -INFINITY ? 0.0f : top;
-                            f[i] = ex2(m[n][i] - ref);
-                            g[i] = ex2(m2 - ref);
+                            const float other_l = red_l[x][n * 8 + quad * 2 + i];
+                            if constexpr (I8) {
+                                const float a_half = ex2(0.5f * (m[n][i] - ref)), b_half = ex2(0.5f * (m2 - ref));
+                                f[i] = a_half * a_half;
+                                g[i] = b_half * b_half;
+                                l[n][i] = l[n][i] * a_half * a_half + other_l * b_half * b_half;
+                            } else {
+                                f[i] = ex2(m[n][i] - ref);
+                                g[i] = ex2(m2 - ref);
+                                l[n][i] = l[n][i] * f[i] + other_l * g[i];
+                            }
                             m[n][i] = top;
-                            l[n][i] = l[n][i] * f[i] + red_l[x][n * 8 + quad * 2 + i] * g[i];
                         }
 #pragma unroll
                         for (int k = 0; k < D / 16; ++k)

@@ -592,7 +592,7 @@ __global__ void __launch_bounds__(threads_of(I8, FORM), 1) tile_kernel(const __g
                     if constexpr (Half2Of<T>::is_bf16) out.v[key] = v;
                     else {
                         const bool some = fabsf(v) >= kLeastScale<T>;
-                        const float size = some ? fabsf(v) : kZeroScale;
+                        const float size = some ? fabsf(v) : kLeastScale<T>;
                         out.v[key] = 1.0f / size;
                         out.v_log[key] = lg2(size);
                         const uint32_t off = __ballot_sync(0xffffffffu, real && !some), neg = __ballot_sync(0xffffffffu, v < 0.0f);

@@ -635,10 +635,10 @@ struct Half2Of<__half> {
 };
 
 // 8-bit pages. Rows whose largest magnitude is below 2^-60 are held as zeros with scale 0, magnitudes beyond 2^60 (f16: 65504) count as that.
-// So a value's scale lies within 2^-67 and 2^53 and may be part of its weight's exponent, 2^(score + log2 scale), without leaving fp32:
-// the sum of the weights, which takes the scale out again, loses nothing that counts. A scale of 0 has no logarithm: its key enters with kZeroScale
-// instead, one of the usual size, and its codes count as 0, as do those of a scale that no append writes because it is smaller than the smallest.
-constexpr float kLeastMagnitude = 8.673617379884035e-19f, kMostBf16 = 1.152921504606847e18f, kMostF16 = 65504.0f, kZeroScale = 0.0078125f;
+// So a value's scale lies within 2^-67 and 2^53 (f16: 2^-31 and 2^9) and may be part of its weight's exponent, 2^(score + log2 scale), without
+// leaving fp32. A scale of 0 has no logarithm: its key enters with the smallest scale instead, which raises no reference that another value
+// needs, and its codes count as 0, as do those of a scale that no append writes because it is smaller than the smallest.
+constexpr float kLeastMagnitude = 8.673617379884035e-19f, kMostBf16 = 1.152921504606847e18f, kMostF16 = 65504.0f;
 template <class T>
 constexpr float kLeastScale = Half2Of<T>::is_bf16 ? 6.776263578034403e-21f : 4.656612873077393e-10f;       // 2^-67; 2^-24 / 127 > 2^-31
 

@@ -27,14 +27,15 @@ def mean_of(s, ref):
     return mean
 
 
-def close(s, got, ref, slack=1e-4, lse_slack=0.0):
-    """Everything relative to the weighted mean of |v|; slack: what the scores may be off by, as they enter a weight."""
+def close(s, got, ref, slack=1e-4, lse_slack=0.0, lost=0.0):
+    """Everything relative to the weighted mean of |v|; slack: what the scores may be off by, as they enter a weight; lost: relative to the row's
+    largest such mean."""
     out, lse = (t.double().cpu() for t in got)
     want, want_lse = ref(s)
     mean = mean_of(s, ref)
     assert torch.isfinite(out).all(), f"{int((~torch.isfinite(out)).sum())} not finite"
     off = (out - want).abs()
-    bad = off > EPS[s.dtype] * (want.abs() + mean) + slack * mean
+    bad = off > EPS[s.dtype] * (want.abs() + mean) + slack * mean + lost * mean.amax(-1, keepdim=True)
     assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} off, worst {float((off / (mean + 1e-300)).max()):.3g} of the mean, at {bad.nonzero()[:3].tolist()}"
     empty = want_lse == -math.inf
     assert torch.equal(lse == -math.inf, empty) and (out[empty] == 0).all()
@@ -275,3 +276,63 @@ def test_switched_off_rows_in_lists(dtype, per_token, q):
     got = S.s3_block_attention(d.cache, d.batch, d.q, lists.cuda(), d.ws, per_token=per_token, want_lse=True)
     d.fine()
     close(s, got, lambda s: R.attention(s, blocks=lists, per_token=per_token))
+
+
+# ---------------------------------------------------------------------------------------------- values far apart
+@pytest.mark.parametrize("dtype,small", [(BF, -50), (BF, -30), (HF, -18)])
+@pytest.mark.parametrize("lens", [[(1, 300), (1, 40)], [(70, 300)], [(300, 400)]])
+@pytest.mark.parametrize("form", [None, dict(cap=20.0)])
+def test_zero_values_beside_small_ones(dtype, small, lens, form):
+    """A value of zeros weighs in the sum and nowhere else: small values beside it keep their bits, whatever their size."""
+    s = R8.Setup8(lens, 8, 2, 128, 16, dtype, seed=3)
+    s.v_scale *= 2.0 ** small
+    zero = torch.randint(0, 3, s.v_scale.shape, generator=s.g) == 0
+    s.v_scale[zero] = 0.0
+    s.v8[zero] = 0
+    d = Device(s)
+    if form is None:
+        got, ref = S.s3_paged_attention(d.cache, d.batch, d.q, d.ws, want_lse=True), lambda s: R.attention(s)
+    else:
+        got, ref = S.s3_paged_attention_scored(d.cache, d.batch, d.q, d.ws, want_lse=True, **form), lambda s: R8.scored(s, **form)
+    d.fine()
+    close_small(s, got, ref)
+
+
+def close_small(s, got, ref):
+    """As `close`, with results so small that the type's smallest number counts beside them."""
+    out, lse = (t.double().cpu() for t in got)
+    want, want_lse = ref(s)
+    mean = mean_of(s, ref)
+    assert ((out - want).abs() <= EPS[s.dtype] * (want.abs() + mean) + 1e-4 * mean + (2.0 ** -25 if s.dtype == HF else 0.0)).all()
+    assert ((lse - want_lse).abs() <= 2e-5 * want_lse.abs().clamp(min=1) + 1e-4).all()
+
+
+@pytest.mark.parametrize("lens", [[(1, 4000), (1, 900)], [(3, 4000)], [(60, 2000)]])
+@pytest.mark.parametrize("order", ["small first", "large first", "mixed"])
+@pytest.mark.parametrize("low,sizes", [(3.0, (56, -58)), (-1.0, (60, -59.5))])
+def test_values_at_both_ends(lens, order, low, sizes):
+    """bf16: most values next to 2^-59, a few next to 2^58, and the many small ones carry most of the weight although each scores lower (base 2:
+    10, 16) than the large: what they add to the sum of weights divides the large ones.
+
+    In a dimension where the large values' codes are 0 nothing is left but the small ones, 2^-110 of the row. Few rows: a weight times its value's
+    scale is an f16 number, at least 2^7 for the row's largest such product, so a key loses at most half of f16's smallest number, 2^-25,
+    hence 2^-32 of that product, times a code of at most 127; 127 times the largest product is no more than the largest mean of |v| over the dimensions
+    (its value has a code of 127 in one of them). So 4000 keys lose 4000 * 2^-32 of that mean."""
+    s = R8.Setup8(lens, 8, 2, 128, 64, seed=4)
+    key = torch.randn(128, generator=s.g)
+    key *= (128 / key.square().sum()).sqrt()
+    s.q = (key + 0.02 * torch.randn(s.q.shape, generator=s.g)).to(BF)
+    for i, (n, kv) in enumerate(s.lens):
+        for x in range(kv):
+            large = {"small first": x == kv - n - 1, "large first": x == 5, "mixed": x % 997 == 500}[order]
+            p = int(s.pages[i, x // 64])
+            k = key * ((10.0 if large else low) / 128 ** 0.5) + 0.05 * torch.randn((2, 128), generator=s.g)
+            s.k8[p, :, x % 64], s.k_scale[p, :, x % 64] = R8.held8(k)
+            v = torch.randn((2, 128), generator=s.g).double()
+            if low < 0:
+                v /= v.abs().amax(-1, keepdim=True)
+            s.v8[p, :, x % 64], s.v_scale[p, :, x % 64] = R8.held8(v * 2.0 ** sizes[0 if large else 1])
+    d = Device(s)
+    got = S.s3_paged_attention(d.cache, d.batch, d.q, d.ws, scale=128 ** -0.5, want_lse=True)
+    d.fine()
+    close(s, got, lambda s: R.attention(s, scale=128 ** -0.5), lost=4000 * 2.0 ** -32)
