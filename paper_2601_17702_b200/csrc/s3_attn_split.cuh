@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
             if (info.rows == 0) break;
             uint32_t q[NT][D / 16][2];
             int qpos[NT][2], qend[NT][2], qown[NT][2];                // position, last visible one, the row's own; the last two for forms
-            float slope[NT][2], q_unit[NT][2];
+            float slope[NT][2], q_unit[NT][2];                        // q_unit, 8-bit pages: factor of the row's products
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 // 8-bit pages: a quad's lane has D / 4 consecutive dimensions of a key, four per product
@@ -324,9 +324,8 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                         for (int x = 0; x < 2; ++x) top = fmaxf(top, fmaxf(fabsf(Half2Of<T>::lo(q[n][k][x])), fabsf(Half2Of<T>::hi(q[n][k][x]))));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                     top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    const int e = static_cast<int>(__float_as_uint(top) >> 23);      // 127 + exponent
-                    const bool usual = e >= 30 && e < 200;             // else as it is: zeros, infinities and numbers next to either
-                    const float up = usual ? __uint_as_float(static_cast<uint32_t>(254 + 14 - e) << 23) : 1.0f;
+                    const int e = static_cast<int>(__float_as_uint(top) >> 23);      // 127 + exponent; 255: an infinity, as it is
+                    const float up = e < 255 ? __uint_as_float(static_cast<uint32_t>(min(254 + 14 - e, 253)) << 23) : 1.0f;
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k)
 #pragma unroll
@@ -334,6 +333,11 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
 #pragma unroll
                     for (int i = 0; i < 2; ++i) q_unit[n][i] = __shfl_sync(0xffffffffu, 1.0f / up, (quad * 2 + i) * 4);
                 } else q_unit[n][0] = q_unit[n][1] = 1.0f;
+                if constexpr (I8) {                                    // with the launch's factor; finite, so that products of 0 stay 0
+                    const float in = FORM ? a.score_in : a.scale_log2;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) q_unit[n][i] = fminf(q_unit[n][i] * in, 3.4e38f);
+                }
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int row = n * 8 + quad * 2 + i;
@@ -401,11 +405,11 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
 #pragma unroll
                                 for (int h = 0; h < 2; ++h) {
                                     const bool real = !edge || (pos_of[u] >= 0 && pos_of[u] + r8 + 8 * h < info.kv);
-                                    const float k_in = real ? scales[16 * u + 8 * h] * a.score_in : 0.0f;
+                                    const float k_scale = real ? scales[16 * u + 8 * h] : 0.0f;
 #pragma unroll
                                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                                        for (int i = 0; i < 2; ++i) z[n * 4 + 2 * h + i] = sc[u][n][2 * h + i] * (k_in * q_unit[n][i]);
+                                        for (int i = 0; i < 2; ++i) z[n * 4 + 2 * h + i] = sc[u][n][2 * h + i] * k_scale * q_unit[n][i];
                                 }
                                 if (a.cap2 > 0.0f) tanh_of_few(z);
 #pragma unroll
@@ -415,7 +419,7 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                             for (int h = 0; h < 2; ++h) {              // keys r8 and r8 + 8
                                 const int kp = pos_of[u] + r8 + 8 * h;
                                 const bool real = !edge || (pos_of[u] >= 0 && kp < info.kv);      // others have codes and scales of any kind
-                                const float k_in = !FORM && real ? scales[16 * u + 8 * h] * a.scale_log2 : 0.0f;
+                                const float k_scale = !FORM && real ? scales[16 * u + 8 * h] : 0.0f;
                                 const float v_scale = real ? scales[TILE + 16 * u + 8 * h] : 0.0f;
                                 const bool some = fabsf(v_scale) >= kLeastScale<T>;
                                 v_log[u][h] = lg2(some ? fabsf(v_scale) : kLeastScale<T>);
@@ -428,7 +432,7 @@ __global__ void __launch_bounds__(THREADS, 2) split_kernel(const __grid_constant
                                         if constexpr (FORM) {
                                             if (a.slopes) y -= slope[n][i] * static_cast<float>(abs(qown[n][i] - kp));
                                             y += v_log[u][h];
-                                        } else y = fmaf(y, k_in * q_unit[n][i], v_log[u][h]);
+                                        } else y = fmaf(y * k_scale, q_unit[n][i], v_log[u][h]);
                                         if (edge && (!real || kp > (FORM ? qend[n][i] : qpos[n][i]) || (a.window > 0 && kp <= qpos[n][i] - a.window))) y = -INFINITY;
                                         grow |= y > m[n][i] + Range::grow;
                                     }

@@ -336,3 +336,32 @@ def test_values_at_both_ends(lens, order, low, sizes):
     got = S.s3_paged_attention(d.cache, d.batch, d.q, d.ws, scale=128 ** -0.5, want_lse=True)
     d.fine()
     close(s, got, lambda s: R.attention(s, scale=128 ** -0.5), lost=4000 * 2.0 ** -32)
+
+
+@pytest.mark.parametrize("q", [1, 3, 60])
+@pytest.mark.parametrize("scale", [2.0 ** -110, 2.0 ** -85, 2.0 ** 100, 1.0 / 16])
+@pytest.mark.parametrize("form", [None, dict(slopes=True), dict(cap=50.0)])
+def test_queries_at_both_ends(q, scale, form):
+    """bf16 rows of 2^111, 2^83 and 2^-105 under scales that bring their scores back (and others', which are then next to 0): powers of two, so that
+    the scores are those of ordinary rows."""
+    if form and form.get("cap") and not 1e-30 <= scale / 50.0 <= 1e30:
+        scale = 2.0 ** -90                                    # the cap's limits
+    s = R8.Setup8([(q, 300)], 8, 2, 128, 16, seed=12)
+    s.q = s.q.float().clamp(-2, 2)
+    for h, e in ((0, 110), (1, 82), (2, -105), (3, 0), (4, 86)):
+        s.q[:, h] *= 2.0 ** e
+    s.q = s.q.to(s.dtype)
+    host = dict(form or {})
+    if host.get("slopes"):
+        host["slopes"] = torch.full((8,), 0.01)
+    dev = {k: v.cuda() if torch.is_tensor(v) else v for k, v in host.items()}
+    d = Device(s)
+    out, lse = (t.double().cpu() for t in S.s3_paged_attention_scored(d.cache, d.batch, d.q, d.ws, scale=scale, want_lse=True, **dev))
+    d.fine()
+    want, want_lse = R8.scored(s, scale=scale, **host)
+    ok = want_lse.abs() < 100                                 # rows whose scores are of ordinary size
+    assert ok.any()
+    mean = mean_of(s, lambda s: R8.scored(s, scale=scale, **host))
+    # scores of up to 100, whose products' magnitudes add up to less than 400: 400 * 2^-21
+    assert ((out - want).abs() <= EPS[s.dtype] * (want.abs() + mean) + 2e-4 * mean)[ok].all()
+    assert ((lse - want_lse).abs() <= 2e-5 * want_lse.abs().clamp(min=1) + 2e-4)[ok].all()
