@@ -365,13 +365,17 @@ __device__ __forceinline__ void shape_scores(float (&s)[32], int c, const Shape&
     }
     if (f.biased) {
         const float away = f.away - 32.0f * c;
+        if (f.capped) {
+#pragma unroll
+            for (int x = 0; x < 32; ++x) s[x] *= f.unit;
+        }
         if (f.ahead) {
 #pragma unroll
-            for (int x = 0; x < 32; ++x) s[x] = fmaf(-f.slope, fabsf(away - x), s[x] * f.unit);
+            for (int x = 0; x < 32; ++x) s[x] = fmaf(-f.slope, fabsf(away - x), s[x]);
         } else {
-            const float base = -f.slope * away;
+            // (the distance first: slope times the tile's distance, rounded once per tile, is off by 2^-24 of 127 slopes beside the row itself)
 #pragma unroll
-            for (int x = 0; x < 32; ++x) s[x] = fmaf(s[x], f.unit, fmaf(f.slope, static_cast<float>(x), base));
+            for (int x = 0; x < 32; ++x) s[x] = fmaf(-f.slope, away - x, s[x]);
         }
     }
     if constexpr (I8 && !Half2Of<T>::is_bf16) {

@@ -365,3 +365,21 @@ def test_queries_at_both_ends(q, scale, form):
     # scores of up to 100, whose products' magnitudes add up to less than 400: 400 * 2^-21
     assert ((out - want).abs() <= EPS[s.dtype] * (want.abs() + mean) + 2e-4 * mean)[ok].all()
     assert ((lse - want_lse).abs() <= 2e-5 * want_lse.abs().clamp(min=1) + 2e-4)[ok].all()
+
+
+@pytest.mark.parametrize("make", [R.Setup, R8.Setup8])
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows", [1, 90, 300])
+@pytest.mark.parametrize("cap", [0.0, 40.0])
+def test_steep_slopes(make, dtype, rows, cap):
+    """Slopes of thousands leave a row its own position and its neighbour's: their scores count the distances 0 and 1, wherever in a tile they lie.
+    The product of a slope and a distance of 1 is off by 2^-24 of itself, next to nothing of a weight that it has made 0. The new rows of the
+    second and third sequence begin at the last position of a tile of keys."""
+    s = make([(rows, 700), (rows, rows + 255), (rows, rows + 127)], 8, 2, 128, 64, dtype, seed=rows)
+    slopes = torch.tensor([0.0, 0.5, 3.0, 30.0, 1000.0, 5000.0, -0.01, 9999.0])
+    d = Device(s)
+    got = S.s3_paged_attention_scored(d.cache, d.batch, d.q, d.ws, cap=cap, slopes=slopes.cuda(), want_lse=True)
+    d.fine()
+    # where more than one key counts slopes are at most 30 and distances below 10: 300 * 2^-23 more. A dimension in which the one key that counts
+    # has a code of 0 holds next to nothing: 700 keys lose up to 700 * 2^-32 there, as in test_values_at_both_ends
+    close(s, got, lambda s: R8.scored(s, cap=cap, slopes=slopes), lost=700 * 2.0 ** -32)
