@@ -82,7 +82,25 @@ __device__ __forceinline__ void normed(F (&x)[16], const float* weight, const Pl
     for (int i = 0; i < 16; ++i) sum += x[i] * x[i];
 #pragma unroll
     for (int o = 1; o < LANES; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    const F inv = F(1) / root(sum / F(D) + F(eps));
+    F add = F(eps);
+    if constexpr (sizeof(F) == 4) {
+        // rows of numbers beyond 2^60, whose squares leave fp32: again, by 2^-70
+        const bool over = !(sum <= 3.4028235e38f);
+        if (__any_sync(0xffffffffu, over)) {
+            const F by = over ? 8.470329472543003e-22f : 1.0f;
+            F again = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                x[i] *= by;
+                again += x[i] * x[i];
+            }
+#pragma unroll
+            for (int o = 1; o < LANES; o <<= 1) again += __shfl_xor_sync(0xffffffffu, again, o);
+            sum = again;
+            add *= by * by;
+        }
+    }
+    const F inv = F(1) / root(sum / F(D) + add);
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
         const float4 w = *reinterpret_cast<const float4*>(weight + (i < 8 ? at.e0 + i : at.e1 + i - 8));

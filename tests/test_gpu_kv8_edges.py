@@ -383,3 +383,30 @@ def test_steep_slopes(make, dtype, rows, cap):
     # where more than one key counts slopes are at most 30 and distances below 10: 300 * 2^-23 more. A dimension in which the one key that counts
     # has a code of 0 holds next to nothing: 700 keys lose up to 700 * 2^-32 there, as in test_values_at_both_ends
     close(s, got, lambda s: R8.scored(s, cap=cap, slopes=slopes), lost=700 * 2.0 ** -32)
+
+
+# ---------------------------------------------------------------------------------------------- norms
+@pytest.mark.parametrize("make", [R.Setup, R8.Setup8])
+@pytest.mark.parametrize("D,rot", [(128, 0), (64, 64)])
+def test_norms_of_rows_of_any_size(make, D, rot):
+    """A norm makes rows of any size alike: bf16 rows from 2^-60 (where eps counts) to 2^126, beside ordinary ones in the same warp. fp32 as in
+    test_gpu_kv8.py: 2^-20 of the row's largest, then one rounding."""
+    s = make([(40, 100), (1, 33)], 4, 2, D, 16, seed=2)
+    sizes = torch.tensor([0, 30, 62, 64, 100, 124, -20, -60, 0, 63])
+    s.q = (s.q.float().clamp(-3, 3) * 2.0 ** sizes[torch.arange(s.T) % 10][:, None, None]).to(BF)
+    s.k = (s.k.float().clamp(-3, 3) * 2.0 ** sizes[torch.arange(s.T) % 10][:, None, None]).to(BF)
+    w = [torch.exp(0.3 * torch.randn(D, generator=s.g)) for _ in range(2)]
+    angle = torch.arange(100, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(0, max(rot, 16), 2, dtype=torch.float64) / max(rot, 16))
+    cos, sin = angle.cos().float(), angle.sin().float()
+    d = Device(s)
+    rope = S.Rope(cos.cuda(), sin.cuda()) if rot else None
+    q = S.s3_kv_append_norm(d.cache, d.batch, s.k.cuda(), s.v.cuda(), d.ws, q=s.q.cuda(), rope=rope, norm=S.HeadNorm(w[0].cuda(), w[1].cuda(), 1e-6))
+    k, _ = S.s3_kv_read(d.cache, d.batch, d.ws)
+    d.fine()
+    for got, x, weight, held in ((q, s.q, w[0], False), (k, s.k, w[1], make is R8.Setup8)):
+        y = R8.new_rows(s, x, weight, 1e-6, cos, sin, rot, False)
+        most = y.abs().amax(-1, keepdim=True)
+        if held:
+            code, scale = R8.held8(y)
+            y = (code.float() * scale[..., None]).double()   # codes are equal, scales within 2^-23
+        assert ((got.double().cpu() - y).abs() <= EPS[BF] * y.abs() + 2.0 ** -19 * most).all()
