@@ -317,17 +317,19 @@ struct Shape {
     float in, unit;                                // factor of the product (16-bit pages); cap in base 2, or 1
     float slope, away;                             // slope (base 2), distance of the row from the tile's first key, negative if it lies before
     bool capped, biased, ahead;                    // ahead: some key lies after some row
+    bool live, whole;                              // the row is there, and all of the tile's keys are
 };
 
-// tanh of scores within 1, two at a time; the same bits as one at a time.
+// tanh by the polynomial of N terms.
+template <int N>
 __device__ __forceinline__ void tanh_of(float (&s)[32])
 {
 #pragma unroll
     for (int x = 0; x < 32; x += 2) {
         const f32x2 z = pair_of(s[x], s[x + 1]), w = fma2(z, z, 0);
-        f32x2 y = pair_of(tanh_part(kTanhParts - 1), tanh_part(kTanhParts - 1));
+        f32x2 y = pair_of(tanh_part<N>(N - 1), tanh_part<N>(N - 1));
 #pragma unroll
-        for (int i = kTanhParts - 2; i >= 0; --i) y = fma2(y, w, pair_of(tanh_part(i), tanh_part(i)));
+        for (int i = N - 2; i >= 0; --i) y = fma2(y, w, pair_of(tanh_part<N>(i), tanh_part<N>(i)));
         split_pair(fma2(y, z, 0), s[x], s[x + 1]);
     }
 }
@@ -354,10 +356,11 @@ __device__ __forceinline__ void shape_scores(float (&s)[32], int c, const Shape&
         float most = 0.0f;
 #pragma unroll
         for (int x = 0; x < 32; x += 2) most = max3(most, fabsf(s[x]), fabsf(s[x + 1]));
-        // The vote also sees keys and rows that do not count, whatever they hold: that may cost time, but changes no bit of a score. (Five terms
-        // where all are within 1/2: 2048 tokens over 16384 keys under a cap of 50 614 us instead of 640, of 30 634 and 639; but then a page's
-        // tail and what another launch left in shared memory chose between two values of the last bits, and to keep them out cost 37 us.)
-        if (__all_sync(0xffffffffu, most <= 1.0f)) tanh_of(s);
+        // What is not there has no say in the form, which shows in the last bits: rows past the tile's (its queries are what another launch has left)
+        // and keys past the last position (16-bit pages: anything, so a tile that has some takes the form that decides score by score; 8-bit
+        // pages: their scales count as 0). NaN takes that form too.
+        if (f.whole && __all_sync(0xffffffffu, most <= 0.5f || !f.live)) tanh_of<5>(s);
+        else if (f.whole && __all_sync(0xffffffffu, most <= 1.0f || !f.live)) tanh_of<7>(s);
         else {
 #pragma unroll
             for (int x = 0; x < 32; ++x) s[x] = tanh_any(s[x]);
@@ -999,7 +1002,7 @@ __global__ void __launch_bounds__(threads_of(I8, FORM), 1) tile_kernel(const __g
                     }
                     const bool capped = bounded || (FORM == FORM_SHAPED && a.cap2 > 0.0f), biased = FORM == FORM_SHAPED && a.slopes;
                     const Shape shape{a.score_in, capped ? a.cap2 : 1.0f, slope, static_cast<float>(info.it.row0 + tok - v0), capped, biased,
-                                      v0 + BN - 1 > info.it.row0 + first_tok};
+                                      v0 + BN - 1 > info.it.row0 + first_tok, live, I8 || v0 + BN <= info.it.kv};
                     const float unit = biased || (I8 && !Half2Of<T>::is_bf16) ? 1.0f : shape.unit;     // that shaping has left to do
                     const uint32_t my_half = my_s + 64 * half;         // its scores, then its weights
                     // Weights that are in place, of chunks before c. Their stores are waited for: nothing else orders a load from tensor memory

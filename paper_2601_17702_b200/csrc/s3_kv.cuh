@@ -571,22 +571,24 @@ __device__ __forceinline__ float lg2(float x)
     asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// tanh(z) / z = sum tanh_part(i) z^2i for |z| <= 1, by the polynomial of degree 6 in z^2 whose largest relative error is smallest (found by the
-// exchange of its extrema): off by 5e-8, evaluated in fp32 below 2e-7. No special function, and exact to the last bits for small z.
-constexpr int kTanhParts = 7;
+// tanh(z) / z = sum tanh_part<N>(i) z^2i, by the polynomial of degree N - 1 in z^2 whose largest relative error is smallest (found by the
+// exchange of its extrema): N = 7 for |z| <= 1, off by 5e-8, N = 5 for |z| <= 1/2, off by 1.3e-8; evaluated in fp32 below 2e-7. No special
+// function, and exact to the last bits for small z.
+template <int N>
 __device__ __forceinline__ constexpr float tanh_part(int i)
 {
+    if (N == 5) return i == 0 ? 9.999999869e-01f : i == 1 ? -3.333306939e-01f : i == 2 ? 1.332477932e-01f : i == 3 ? -5.298607529e-02f : 1.713500663e-02f;
     return i == 0 ? 9.999999502e-01f : i == 1 ? -3.333283915e-01f : i == 2 ? 1.332520408e-01f : i == 3 ? -5.345702956e-02f : i == 4 ? 2.028998042e-02f
          : i == 5 ? -6.203379098e-03f : 1.041022631e-03f;
 }
-// tanh(z) is that for |z| <= 1, else by tanh(z) = 1 - 2 / (1 + e^2z), which is off by 2^-22: of little beside the result where |z| > 1, of all of it
+// tanh(z) is that of seven terms for |z| <= 1, else by tanh(z) = 1 - 2 / (1 + e^2z), which is off by 2^-22: of little beside the result where |z| > 1, of all of it
 // where z is small (a cap of 1e6 over scores of 2 takes every z there).
 __device__ __forceinline__ float tanh_near(float z)
 {
     const float w = z * z;
-    float y = tanh_part(kTanhParts - 1);
+    float y = tanh_part<7>(6);
 #pragma unroll
-    for (int i = kTanhParts - 2; i >= 0; --i) y = fmaf(y, w, tanh_part(i));
+    for (int i = 5; i >= 0; --i) y = fmaf(y, w, tanh_part<7>(i));
     return y * z;
 }
 __device__ __forceinline__ float tanh_far(float z) { return fmaf(-2.0f, rcp(1.0f + ex2(2.0f * kLog2e * z)), 1.0f); }
