@@ -24,11 +24,11 @@
 // the tensor pipe busy 62 % and that of the exponentials 65 % of the time; 7 ragged chunks of up to 733 tokens at head_dim 64
 // 72 us, where the units' starts and ends show.
 //
-// 8-bit pages: the same chunk over 32768 keys 1290 us (f16 rows 1420). Widening 32 K codes a tile is hidden; what shows is the reading of the
+// 8-bit pages: the same chunk over 32768 keys 1293 us (f16 rows 1456). Widening 32 K codes a tile is hidden; what shows is the reading of the
 // scales, four LDS per four keys and row with few registers to read ahead (the first half's weights take 2650 cycles of 5630 a tile, 1050
-// over 16-bit pages). Capped, 2048 tokens over 16384 keys: 632 us (f16, with references: 798) against 424 plain; with references the multiply-add
-// pipes are half busy, and a group waits 1450 of 6900 cycles a tile for its scores, since both groups are in step (half a turn apart they
-// took as long). Instructions count: six copies of the widening loop instead of one cost 40 % (instruction cache).
+// over 16-bit pages). Capped, 2048 tokens over 16384 keys: 653 us (cap 30; 50, where five terms of tanh suffice, 629; f16, with references: 812) against 413 plain; with
+// references the multiply-add pipes are half busy, and a group waits 1450 of 6900 cycles a tile for its scores, since both groups are in
+// step (half a turn apart they took as long). Instructions count: six copies of the widening loop instead of one cost 40 % (instruction cache).
 //
 // Every mbarrier wait is bounded; one that runs out sets the status word and the block's abort flag, and the block waits for its
 // copies and frees its tensor memory before it leaves.
@@ -57,7 +57,7 @@ constexpr int TMEM_COLS = 512;
 // leaves bf16), and where all of a row's scores are low, small values vanish. Neither happens with numbers of ordinary size, and both
 // show in the results: a block that finds one that is not finite, or a sum of weights below kLeastSum, marks itself, and a second launch of the
 // same grid makes its results again with references; the other blocks leave at once (2 to 9 us a call; with references throughout 32 tokens
-// over 300 keys take 18.8 us against 17.9, 512 over 4096 75 against 68, 2048 over 16384 759 against 650). At a sum of kLeastSum or more, what products below
+// over 300 keys take 20.0 us against 17.9, 512 over 4096 74 against 63, 2048 over 16384 755 against 635). At a sum of kLeastSum or more, what products below
 // fp32's normal numbers lose is less than 2^-102 a key.
 enum { FORM_NONE = 0, FORM_PREFIX = 1, FORM_SHAPED = 2, FORM_BOUNDED = 3 };
 constexpr float kBoundedCap = 80.0f;       // base 2
@@ -318,6 +318,7 @@ struct Shape {
     float slope, away;                             // slope (base 2), distance of the row from the tile's first key, negative if it lies before
     bool capped, biased, ahead;                    // ahead: some key lies after some row
     bool live, whole;                              // the row is there, and all of the tile's keys are
+    int tail;                                      // keys of the tile that are there
 };
 
 // tanh by the polynomial of N terms.
@@ -357,11 +358,12 @@ __device__ __forceinline__ void shape_scores(float (&s)[32], int c, const Shape&
 #pragma unroll
         for (int x = 0; x < 32; x += 2) most = max3(most, fabsf(s[x]), fabsf(s[x + 1]));
         // What is not there has no say in the form, which shows in the last bits: rows past the tile's (its queries are what another launch has left)
-        // and keys past the last position (16-bit pages: anything, so a tile that has some takes the form that decides score by score; 8-bit
-        // pages: their scales count as 0). NaN takes that form too.
-        if (f.whole && __all_sync(0xffffffffu, most <= 0.5f || !f.live)) tanh_of<5>(s);
-        else if (f.whole && __all_sync(0xffffffffu, most <= 1.0f || !f.live)) tanh_of<7>(s);
-        else {
+        // and keys past the last position (16-bit pages: anything, so that scores some of which are of such keys take the form that decides one by
+        // one; 8-bit pages: their scales count as 0). NaN takes that form too.
+        const bool whole = f.whole || f.tail >= 32 * c + 32;
+        if (whole && __all_sync(0xffffffffu, most <= 0.5f || !f.live)) tanh_of<5>(s);
+        else if (whole && __all_sync(0xffffffffu, most <= 1.0f || !f.live)) tanh_of<7>(s);
+        else if (f.tail > 32 * c) {
 #pragma unroll
             for (int x = 0; x < 32; ++x) s[x] = tanh_any(s[x]);
         }
@@ -993,7 +995,7 @@ __global__ void __launch_bounds__(threads_of(I8, FORM), 1) tile_kernel(const __g
                 if constexpr (SHAPED) {
                     // Shaped scores: two threads per row, 64 keys each. Shaping adds as much to a score as its weight costs, nothing of it waits for
                     // anything else, and what bounds eight warps then is the latency of their instructions: capped, 2048 tokens over 16384 keys,
-                    // 888 us with one thread per row and 757 with two. The two share the row's reference. It stays as it is unless a weight may be too large for it, or there is
+                    // with references, 888 us with one thread per row and 757 with two. The two share the row's reference. It stays as it is unless a weight may be too large for it, or there is
                     // none yet: the thread that finds one goes on with a reference of its own, and before the weights are handed over both
                     // take the larger one and bring what they made with another, and half of the accumulator each, along.
                     if constexpr (I8) {
@@ -1002,7 +1004,7 @@ __global__ void __launch_bounds__(threads_of(I8, FORM), 1) tile_kernel(const __g
                     }
                     const bool capped = bounded || (FORM == FORM_SHAPED && a.cap2 > 0.0f), biased = FORM == FORM_SHAPED && a.slopes;
                     const Shape shape{a.score_in, capped ? a.cap2 : 1.0f, slope, static_cast<float>(info.it.row0 + tok - v0), capped, biased,
-                                      v0 + BN - 1 > info.it.row0 + first_tok, live, I8 || v0 + BN <= info.it.kv};
+                                      v0 + BN - 1 > info.it.row0 + first_tok, live, I8 || v0 + BN <= info.it.kv, info.it.kv - v0};
                     const float unit = biased || (I8 && !Half2Of<T>::is_bf16) ? 1.0f : shape.unit;     // that shaping has left to do
                     const uint32_t my_half = my_s + 64 * half;         // its scores, then its weights
                     // Weights that are in place, of chunks before c. Their stores are waited for: nothing else orders a load from tensor memory
