@@ -18,10 +18,10 @@
 //
 // 8-bit pages (I8): codes and scales are copied as they are, half the bytes, and widened in registers on the way into the products (f16,
 // exactly). The operands take the order in which the bytes lie: the dimensions of a key may be summed in any order, so a lane's 16-byte
-// pieces are its part of K as they come, and V's rows are dimensions, so any lane may have any of them. Bound by instructions as much
-// as by memory: 360 per 16 keys, four warps per block. So a warp takes 32 keys a step, which gives the products and exponentials of two groups to
-// overlap (one group: 68 us for one token over 131072 keys, two: 60; three or four blocks per SM with one: 64, 63; floor 43 and about 8 for
-// the launch's start, its end and the join).
+// pieces are its part of K as they come, and V's rows are dimensions, so any lane may have any of them. Bound by
+// latency: some 370 instructions per 16 keys by two warps per scheduler, which issue in 41 % of the cycles. So a warp takes 32 keys a step, which
+// gives the products and exponentials of two groups to overlap (one group: 68 us for one token over 131072 keys, two: 60; three or four blocks
+// per SM with one: 64, 63; floor 43 and about 8 for the launch's start, its end and the join).
 #pragma once
 
 #include <string.h>
