@@ -410,3 +410,15 @@ def test_norms_of_rows_of_any_size(make, D, rot):
             code, scale = R8.held8(y)
             y = (code.float() * scale[..., None]).double()   # codes are equal, scales within 2^-23
         assert ((got.double().cpu() - y).abs() <= EPS[BF] * y.abs() + 2.0 ** -19 * most).all()
+
+
+@pytest.mark.parametrize("make", [R.Setup, R8.Setup8])
+def test_a_workspace_of_the_header_alone(make):
+    """Calls that take whole units need no more; what is not there to mark blocks in is not written."""
+    s = make([(20, 200), (30, 90)], 8, 2, 128, 64, seed=6)
+    d = Device(s)
+    pool = torch.zeros(4096, dtype=torch.uint8, device="cuda")
+    pool[64:] = 171
+    got = S.s3_paged_attention_scored(d.cache, d.batch, d.q, pool[:64], cap=30.0, want_lse=True)
+    close(s, got, lambda s: R8.scored(s, cap=30.0))
+    assert (pool[64:] == 171).all() and S.s3_workspace_status(pool[:64]) == 0
