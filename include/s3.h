@@ -604,8 +604,9 @@ s3_status s3_kv_cache_destroy(s3_kv_cache* cache);
  * them, in 64 bits and not rounded to the rows' type before; ties go to the even code. Every call below takes such a cache; summaries are of
  * the keys that the codes stand for. Where a call reads positions < kv_len of a block, their scales must be finite; they may have
  * either sign. A caller who writes value scales keeps them at 0 or within [2^-67, 2^53] in magnitude (S3_F16: [2^-31, 2^9], what an append writes);
- * attention may take a smaller one for 0. Queries lie within 2^112 (their products with codes are summed in fp32). Attention in f16, and of few rows in either type, rounds a weight times its value's scale to f16, at 2^7 or
- * more for the row's largest such product: what a key adds may be off by 2^-32 of the row's largest addition. */
+ * attention may take a smaller one for 0. Queries lie within 2^112 (their products with codes are summed in fp32). Attention in f16, and of
+ * few rows in either type, rounds a weight times its value's scale to f16, at 2^7 or more for the row's largest such product: what a key adds
+ * may be off by 2^-32 of the row's largest addition (values of zeros count there with the smallest scale). */
 s3_status s3_kv_cache_create_i8(s3_kv_cache** out, const s3_kv_cache_desc* desc, float* d_k_scale, float* d_v_scale);
 /* Scratch that suffices for every call over this batch (or one with smaller bounds) with n_heads query heads. */
 size_t s3_kv_workspace_bytes(const s3_kv_cache* cache, const s3_kv_batch* batch, int n_heads);
